@@ -62,13 +62,14 @@ typedef enum {
   GSI_ERR_WORKSPACE = 6    /* workspace smaller than gsi_workspace_bytes()          */
 } gsi_status_t;
 
-typedef enum { GSI_BF16 = 0, GSI_F32 = 1 } gsi_dtype_t;
+typedef enum { GSI_BF16 = 0, GSI_F32 = 1, GSI_F16 = 2 /* cache calls only */ } gsi_dtype_t;
 
 /* A CUDA stream (cudaStream_t), spelt without the CUDA headers. */
 typedef struct CUstream_st* gsi_stream_t;
 
 typedef struct gsi_layer* gsi_handle_t; /* one group */
 typedef struct gsi_stack* gsi_stack_t;  /* an ordered chain of groups */
+typedef struct gsi_kv* gsi_kv_t;        /* a cache of keys and values in 4 bits */
 
 enum {
   GSI_FLAG_NONE = 0u,
@@ -432,6 +433,128 @@ gsi_status_t gsi_stack_step_host(gsi_stack_t s, const float* const* x_host_array
  */
 gsi_status_t gsi_stack_get_status(gsi_stack_t s, int* device_status);
 gsi_status_t gsi_stack_destroy(gsi_stack_t s);
+
+/* ------------------------------------------------------------------------ *
+ * Keys and values in 4 bits, in pages, and attention over them: what lies
+ * between the group of a block that makes q, k and v (columns of its y) and the
+ * group that takes the attention's output (its x).
+ *
+ * Numbers.  For every token and head, 64 channels at a time (the last ones of a
+ * head may be fewer):
+ *   s    = f16((max - min) (1/15))   saturating at 65504; 1/15 rounded to fp32
+ *   mid  = f16(min + 8 s)            saturating at +-65504
+ *   code = clamp(rint((x - mid) / s) + 8, 0, 15), 8 where s = 0
+ *   value = s (code - 8) + mid
+ * every step a single fp32 operation, conversions to nearest even.  Where one of
+ * the 64 is not finite, s = mid = NaN, and all of them read as NaN.  So an element
+ * is off by s / 2 and the rounding of mid, 2^-11 |mid| at most (and by 2^-11 of
+ * 8 s from the rounding of s, where codes clamp).
+ *
+ * Pages.  A pool is n_pages pages of gsi_kv_page_bytes(); each holds page_tokens
+ * tokens of all heads: [head][tile of 16 tokens][K, V][64 channels] blocks of
+ * 576 bytes, 512 of codes in the order of the tensor cores' operand, then the 16
+ * pairs (s, mid); gsi_kv_locate gives the place of every element.  A slot is
+ * page * page_tokens + token within the page.  One handle serves the pools of
+ * all layers: every layer's pool has the same pages in use.
+ *
+ * State (device, caller-owned): lens [max_seqs] tokens of each sequence in the
+ * cache; table [max_seqs][max_pages] the pages of each, in order; free_pages
+ * [n_pages], of which the first *n_free are the pages that nobody holds (at the
+ * start all of them, *n_free = n_pages, lens = 0).
+ *
+ * A step: gsi_kv_plan once; per layer gsi_kv_append, gsi_kv_attend; then, for
+ * sequences that have ended, gsi_kv_release.  Nothing of it is read on the host, so a
+ * whole step can be captured into a CUDA graph.  The calls run on the device
+ * that was current at gsi_kv_create (GSI_ERR_INVALID_ARG with another one
+ * current), do not synchronise and allocate nothing.  One handle may be used by
+ * one stream at a time, graphs that hold its calls included.
+ * ------------------------------------------------------------------------ */
+
+#define GSI_KV_MAX_SEQS 2048
+#define GSI_KV_MAX_DIM 256
+
+typedef struct {
+  int n_heads;     /* heads of K and V                                              */
+  int head_dim;    /* channels of a head, 1..GSI_KV_MAX_DIM                         */
+  int page_tokens; /* a multiple of 16, up to 4096                                  */
+  int n_pages;     /* pages of a pool; n_pages * page_tokens < 2^31                 */
+  int max_seqs;    /* 1..GSI_KV_MAX_SEQS                                            */
+  int max_pages;   /* pages of one sequence: the table's row; max_pages * page_tokens < 2^31 */
+  int max_tokens;  /* new tokens of a step: the length of slots and positions       */
+} gsi_kv_desc_t;
+
+/* Bytes of one page of one pool, of the workspace (0 if desc is invalid). */
+size_t gsi_kv_page_bytes(const gsi_kv_desc_t* desc);
+size_t gsi_kv_workspace_bytes(const gsi_kv_desc_t* desc);
+
+/* Place of channel `channel` of head `head` of the token in `slot`, for K (is_v = 0) or V (1), in
+ * bytes from the pool's first: the byte that holds its code (the lower half of it for an even channel,
+ * the upper half for an odd one) and the four bytes that hold its pair (s, then mid).  Host only. */
+gsi_status_t gsi_kv_locate(const gsi_kv_desc_t* desc, int slot, int head, int channel, int is_v,
+                           size_t* code_byte_out, size_t* pair_byte_out);
+
+/* workspace: device memory, 256-byte aligned, the handle's alone until gsi_kv_destroy.  Synchronises `stream`. */
+gsi_status_t gsi_kv_create(const gsi_kv_desc_t* desc, void* workspace, size_t workspace_bytes,
+                           gsi_stream_t stream, gsi_kv_t* out);
+
+/*
+ * Room for n_new[s] >= 0 more tokens of sequence s, s < n_seqs <= max_seqs, in order: pages are taken
+ * from the end of the free ones, page j of the step is free_pages[*n_free - 1 - j].  Writes
+ *   table      the new pages, behind those that a sequence has
+ *   q_start    [n_seqs + 1]  the first row of each sequence's new tokens among those of the step
+ *   kv_len     [n_seqs]      its tokens with the new ones; 0 if it was refused
+ *   slots      [max_tokens]  the slot of each new token; -1 if refused, and behind the last one
+ *   positions  [max_tokens]  its place in its sequence; -1 likewise
+ *   counts     [4]           new tokens, pages taken, pages left, sequences refused
+ * Refused, and left as it was, is a sequence that needs a page where the pages asked for up to and with it
+ * are more than the free ones (those behind it that need none are served), one that would be longer than its
+ * table's row, one whose rows end behind max_tokens, one with n_new < 0 (which counts as no rows).
+ * commit = 1: lens and *n_free move on.  commit = 0: they stay, so the next plan hands out the same pages
+ * again (a step that may be taken back).  One launch.
+ */
+gsi_status_t gsi_kv_plan(gsi_kv_t h, const int* n_new, int n_seqs, int commit, int* lens, int* n_free,
+                         const int* free_pages, int* table, int* q_start, int* kv_len, int* slots,
+                         int* positions, int* counts, gsi_stream_t stream);
+
+/* Sequences with done[s] != 0 give their pages back (so that a plan for empty sequences and a release of
+ * them leave the free pages as they were), their table rows become -1 and their lens 0.  One launch. */
+gsi_status_t gsi_kv_release(gsi_kv_t h, const unsigned char* done, int n_seqs, int* lens, int* n_free,
+                            int* free_pages, int* table, gsi_stream_t stream);
+
+/*
+ * k, v: n_tokens rows of n_heads x head_dim, of `dtype`; strides in elements, channels adjacent.  Row i goes
+ * to slots[i]; a negative slot is passed over, one behind the pool too, which the status word reports
+ * (GSI_ERR_INVALID_ARG).  Slots that are not passed over are distinct.  One launch.
+ */
+gsi_status_t gsi_kv_append(gsi_kv_t h, const void* k, const void* v, gsi_dtype_t dtype, int64_t k_token_stride,
+                           int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                           const int* slots, int n_tokens, void* pages, gsi_stream_t stream);
+
+/* The values in n slots, to k_out and v_out [n][n_heads][head_dim] of `dtype`; zeros for a slot that
+ * gsi_kv_append passes over. */
+gsi_status_t gsi_kv_read(gsi_kv_t h, const void* pages, const int* slots, int n, gsi_dtype_t dtype, void* k_out,
+                         void* v_out, gsi_stream_t stream);
+
+/*
+ * Attention of the step's rows: row i of sequence s (rows q_start[s] .. q_start[s + 1] - 1, m of them) sees
+ * the tokens 0 .. kv_len[s] - m + i of its sequence, its own among them, and
+ *   out = sum_p softmax_p(scale q . k_p) v_p        0 where it sees none
+ * q, out: n_rows rows of n_q_heads x head_dim of `dtype`, n_q_heads a multiple of n_heads: q head j goes with
+ * head j / (n_q_heads / n_heads).  Strides in elements, channels adjacent, >= 0 (out's rows apart from each
+ * other).  Rows behind the last sequence's are left as they were.  Softmax and sums are held in fp32; the contractions
+ * take q and the probabilities rounded to 22 bits for fp32, to 11 for 16-bit types.  A page number outside the
+ * pool, or a length outside the table, is reported by the status word (GSI_ERR_INVALID_ARG) and gives
+ * NaN in the rows that would see it.  Which sums are made where follows from the lengths; a call is reproducible
+ * bit for bit.
+ */
+gsi_status_t gsi_kv_attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t q_token_stride,
+                           int64_t q_head_stride, int n_rows, int n_q_heads, float scale, const int* q_start,
+                           const int* kv_len, const int* table, int n_seqs, const void* pages, void* out,
+                           int64_t out_token_stride, int64_t out_head_stride, gsi_stream_t stream);
+
+/* Synchronises the handle's last stream and returns the status word, which stays set. */
+gsi_status_t gsi_kv_get_status(gsi_kv_t h, int* device_status);
+gsi_status_t gsi_kv_destroy(gsi_kv_t h);
 
 #ifdef __cplusplus
 }

@@ -14,9 +14,10 @@ import torch
 
 from . import build as _build
 
-GSI_BF16, GSI_F32 = 0, 1
+GSI_BF16, GSI_F32, GSI_F16 = 0, 1, 2
 GSI_FLAG_NONE, GSI_FLAG_STATIC_PROJECTION, GSI_FLAG_DENSE, GSI_FLAG_FP8_IMAGE = 0, 1, 2, 4
 GSI_MAX_MAPS, GSI_MAX_TOKENS = 8, 64
+GSI_KV_MAX_SEQS, GSI_KV_MAX_DIM = 2048, 256
 
 EXPORTED = [
     "gsi_status_string", "gsi_build_image", "gsi_workspace_bytes", "gsi_create",
@@ -24,6 +25,8 @@ EXPORTED = [
     "gsi_set_spin_limit", "gsi_destroy", "gsi_stack_workspace_bytes", "gsi_stack_create", "gsi_stack_bind",
     "gsi_stack_set_mode", "gsi_stack_set_concurrent", "gsi_stack_is_persistent", "gsi_stack_set_trace", "gsi_stack_set_spin_limit", "gsi_stack_seek", "gsi_stack_step", "gsi_stack_launches_per_step",
     "gsi_stack_step_host", "gsi_stack_get_status", "gsi_stack_destroy",
+    "gsi_kv_page_bytes", "gsi_kv_workspace_bytes", "gsi_kv_locate", "gsi_kv_create", "gsi_kv_plan", "gsi_kv_release",
+    "gsi_kv_append", "gsi_kv_read", "gsi_kv_attend", "gsi_kv_get_status", "gsi_kv_destroy",
 ]
 
 
@@ -35,6 +38,10 @@ class GsiDesc(C.Structure):
 
 class GsiStackIo(C.Structure):
     _fields_ = [("x", C.c_void_p), ("y", C.c_void_p)]
+
+
+class GsiKvDesc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("n_heads", "head_dim", "page_tokens", "n_pages", "max_seqs", "max_pages", "max_tokens")]
 
 
 class GsiError(RuntimeError):
@@ -83,8 +90,21 @@ def _load():
     l.gsi_stack_step_host.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), vp, vp]
     l.gsi_stack_get_status.argtypes = [vp, C.POINTER(i)]
     l.gsi_stack_destroy.argtypes = [vp]
+    kd, ll = C.POINTER(GsiKvDesc), C.c_longlong
+    l.gsi_kv_page_bytes.restype = l.gsi_kv_workspace_bytes.restype = sz
+    l.gsi_kv_page_bytes.argtypes = l.gsi_kv_workspace_bytes.argtypes = [kd]
+    l.gsi_kv_locate.argtypes = [kd, i, i, i, i, C.POINTER(sz), C.POINTER(sz)]
+    l.gsi_kv_create.argtypes = [kd, vp, sz, vp, C.POINTER(vp)]
+    l.gsi_kv_plan.argtypes = [vp, vp, i, i, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    l.gsi_kv_release.argtypes = [vp, vp, i, vp, vp, vp, vp, vp]
+    l.gsi_kv_append.argtypes = [vp, vp, vp, i, ll, ll, ll, ll, vp, i, vp, vp]
+    l.gsi_kv_read.argtypes = [vp, vp, vp, i, i, vp, vp, vp]
+    l.gsi_kv_attend.argtypes = [vp, vp, i, ll, ll, i, i, C.c_float, vp, vp, vp, i, vp, vp, ll, ll, vp]
+    l.gsi_kv_get_status.argtypes = [vp, C.POINTER(i)]
+    l.gsi_kv_destroy.argtypes = [vp]
     for name in EXPORTED:
-        if name not in ("gsi_status_string", "gsi_workspace_bytes", "gsi_stack_workspace_bytes"):
+        if name not in ("gsi_status_string", "gsi_workspace_bytes", "gsi_stack_workspace_bytes", "gsi_kv_page_bytes",
+                        "gsi_kv_workspace_bytes"):
             getattr(l, name).restype = i
     return l
 
@@ -95,6 +115,8 @@ def _load_calls():
     m = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(m)
     m.bind(*[C.cast(f, C.c_void_p).value for f in (lib.gsi_forward_n, lib.gsi_extend_basis, lib.gsi_forward_static)])
+    m.bind_kv(*[C.cast(f, C.c_void_p).value for f in (lib.gsi_kv_plan, lib.gsi_kv_release, lib.gsi_kv_append, lib.gsi_kv_read,
+                                                      lib.gsi_kv_attend)])
     return m
 
 
@@ -359,6 +381,119 @@ class Stack:
     def close(self):
         if getattr(self, "handle", None):
             lib.gsi_stack_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class KVCache:
+    """Keys and values in 4 bits, in pages, for up to ``max_seqs`` requests of up to ``max_len`` tokens, and
+    attention over them (``include/gsi.h`` has the numbers' definition and the pages' layout).
+
+        cache.plan(n_new)                         # once a step: pages, slots and positions of the new tokens
+        cache.append(k, v, layer)                 # per layer: k, v [n][n_heads][head_dim], as columns of a group's y
+        out = cache.attend(q, layer)              # q, out [n][q heads][head_dim]
+        cache.release(done)                       # requests that have ended give their pages back
+
+    Device tensors: the state ``lens``, ``table``, ``free``, ``n_free``, and what a plan leaves, ``q_start``,
+    ``kv_len``, ``slots``, ``positions``, ``counts`` (new tokens, pages taken, pages left, requests refused).  None is
+    read on the host, so a step can be captured into a CUDA graph.  ``pages`` (uint8, [n_layers][n_pages][bytes of a
+    page]) may be the caller's memory.  One cache may be used by one stream at a time.
+    """
+
+    def __init__(self, n_heads: int, head_dim: int, n_pages: int, max_seqs: int, max_len: int, page_tokens: int = 64,
+                 n_layers: int = 1, max_tokens: int = GSI_MAX_TOKENS, device="cuda", pages: torch.Tensor | None = None,
+                 stream=None):
+        self.n_heads, self.head_dim, self.n_pages, self.page_tokens = int(n_heads), int(head_dim), int(n_pages), int(page_tokens)
+        self.n_layers = int(n_layers)
+        max_pages = -(-int(max_len) // max(1, self.page_tokens))
+        self._desc = GsiKvDesc(self.n_heads, self.head_dim, self.page_tokens, self.n_pages, int(max_seqs), max_pages, int(max_tokens))
+        self.page_bytes, nbytes = int(lib.gsi_kv_page_bytes(C.byref(self._desc))), int(lib.gsi_kv_workspace_bytes(C.byref(self._desc)))
+        if nbytes == 0 or self.n_layers < 1:
+            raise GsiError(2, "gsi_kv_workspace_bytes (descriptor rejected)")
+        dev = torch.device(device) if pages is None else pages.device
+        assert dev.type == "cuda", "the cache lives on a CUDA device"
+        if dev.index is None:
+            dev = torch.device("cuda", torch.cuda.current_device())
+        whole = self.n_layers * self.n_pages * self.page_bytes
+        if pages is None:
+            pages = torch.empty((self.n_layers, self.n_pages, self.page_bytes), dtype=torch.uint8, device=dev)
+        assert pages.dtype == torch.uint8 and pages.is_contiguous() and pages.numel() == whole and pages.data_ptr() % 16 == 0
+        self.device, self.pages = dev, pages
+
+        def ints(*shape, fill=0):
+            return torch.full(shape, fill, dtype=torch.int32, device=dev)
+
+        with torch.cuda.device(dev):
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            self.table, self.lens = ints(int(max_seqs), max_pages, fill=-1), ints(int(max_seqs))
+            self.free = torch.arange(self.n_pages - 1, -1, -1, dtype=torch.int32, device=dev)
+            self.n_free = ints(1, fill=self.n_pages)
+            self.q_start, self.kv_len = ints(int(max_seqs) + 1), ints(int(max_seqs))
+            self.slots, self.positions = ints(int(max_tokens), fill=-1), ints(int(max_tokens), fill=-1)
+            self.counts = ints(4)
+            h = C.c_void_p()
+            _check(lib.gsi_kv_create(C.byref(self._desc), self.workspace.data_ptr(), nbytes, _stream_ptr(stream), C.byref(h)), "gsi_kv_create")
+        self.handle = h
+        self._state = _calls.kv_state(h.value, self.n_heads, self.head_dim, self.n_layers, pages, self.table, self.lens, self.free,
+                                      self.n_free, self.q_start, self.kv_len, self.slots, self.positions, self.counts)
+        self._like = {t: torch.empty(0, dtype=t) for t in (torch.float32, torch.bfloat16, torch.float16)}
+        self._scale = float(self.head_dim) ** -0.5
+
+    def plan(self, n_new: torch.Tensor, commit: bool = True, stream=None):
+        """Room for ``n_new[s]`` more tokens of request s (int32, device), one launch.  ``commit=False`` leaves
+        ``lens`` and ``n_free`` as they are: the next plan hands out the same pages again."""
+        status = _calls.kv_plan(self._state, n_new, commit, stream)
+        if status:
+            _check(status, "gsi_kv_plan")
+
+    def release(self, done: torch.Tensor, stream=None):
+        """Requests s with ``done[s]`` (bool or uint8, device) give their pages back and are empty."""
+        status = _calls.kv_release(self._state, done, stream)
+        if status:
+            _check(status, "gsi_kv_release")
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, layer: int = 0, slots: torch.Tensor | None = None, stream=None):
+        """Row i of k and v to ``slots[i]`` (the plan's by default), rows with a negative slot nowhere."""
+        status = _calls.kv_append(self._state, k, v, layer, slots, stream)
+        if status:
+            _check(status, "gsi_kv_append")
+
+    def attend(self, q: torch.Tensor, layer: int = 0, scale: float | None = None, out: torch.Tensor | None = None, stream=None):
+        """Attention of the plan's rows, each over its request's tokens up to its own; ``scale`` is
+        ``head_dim ** -0.5`` by default.  Rows behind the last request's are not written."""
+        status, out = _calls.kv_attend(self._state, q, layer, self._scale if scale is None else scale, out, stream)
+        if status:
+            _check(status, "gsi_kv_attend")
+        return out
+
+    def read(self, slots: torch.Tensor, layer: int = 0, dtype: torch.dtype = torch.float32, stream=None):
+        """(k, v) [n][n_heads][head_dim]: the values that ``slots`` (int32, device) hold, zeros for a negative one."""
+        status, k, v = _calls.kv_read(self._state, slots, layer, self._like[dtype], stream)
+        if status:
+            _check(status, "gsi_kv_read")
+        return k, v
+
+    def locate(self, slot: int, head: int, channel: int, is_v: bool):
+        """(byte of the code, byte of the pair) of one element, from the first of a layer's pages."""
+        code, pair = C.c_size_t(), C.c_size_t()
+        _check(lib.gsi_kv_locate(C.byref(self._desc), slot, head, channel, int(is_v), C.byref(code), C.byref(pair)), "gsi_kv_locate")
+        return code.value, pair.value
+
+    def status(self) -> int:
+        v = C.c_int()
+        with torch.cuda.device(self.device):
+            _check(lib.gsi_kv_get_status(self.handle, C.byref(v)), "gsi_kv_get_status")
+        return v.value
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _calls.kv_close(self._state)
+            lib.gsi_kv_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

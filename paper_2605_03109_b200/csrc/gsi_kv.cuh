@@ -1,0 +1,95 @@
+// Keys and values in 4 bits: the pages' layout and what the kernels of a cache take (gsi_kv.cu, gsi_kv_attend.cu).
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "gsi_common.cuh"
+
+namespace gsi {
+namespace kv {
+
+constexpr int kTile = 16;          // tokens of a tile
+constexpr int kGroup = 64;         // channels that share a pair (s, mid)
+constexpr int kCodeBytes = 512;    // codes of a block: 16 tokens x 64 channels, 16 bytes a lane of a warp
+constexpr int kBlockBytes = 576;   // ... and 16 pairs
+constexpr int kMaxCtas = 320;      // of the attention's grid: what the workspace has room for
+constexpr int kMaxRows = 16;       // rows of the attention that a CTA takes at a time
+
+// Layout within a block, of token t (0..15) and channel c (0..63).  K is the A operand of m16n8k16 with tokens as
+// its rows: lane 4 (t % 8) + c / 16 holds 16 channels of tokens t % 8 and t % 8 + 8.  V is the A operand with
+// channels as its rows and tokens as the contraction: the two halves of a 32-bit word are the tokens of a pair,
+// so that a mask takes the same channel of both, and lane 4 (c / 8) + t % 8 / 2 holds 8 channels of four tokens.
+__host__ __device__ __forceinline__ int k_byte(int t, int c) { return ((t % 8) * 4 + c / 16) * 16 + (t / 8) * 8 + c % 16 / 2; }
+__host__ __device__ __forceinline__ int v_byte(int t, int c) {
+  return ((c / 8) * 4 + t % 8 / 2) * 16 + (t / 8) * 8 + c % 8 / 4 * 4 + t % 2 * 2 + c % 4 / 2;
+}
+__host__ __device__ __forceinline__ int pair_byte(int t) { return kCodeBytes + (2 * (t % 8) + t / 8) * 4; }
+
+struct Shape {
+  int n_heads, head_dim, groups, page_tokens, page_tiles, n_pages, max_seqs, max_pages, max_tokens;
+  long long tile_bytes, head_bytes, page_bytes;   // a tile of a head (K and V), a head of a page, a page
+};
+
+// First byte of tile `tile` of a head in a page.
+__host__ __device__ __forceinline__ long long tile_at(const Shape& s, int page, int head, int tile) {
+  return page * s.page_bytes + head * s.head_bytes + tile * s.tile_bytes;
+}
+
+struct Control {          // at the front of the workspace
+  int status;
+  unsigned plan_ticket;   // blocks of a plan or release that have read its state
+};
+
+struct PlanArgs {
+  const int* n_new;
+  int n_seqs, commit;
+  int *lens, *n_free;
+  const int* free_pages;
+  int *table, *q_start, *kv_len, *slots, *positions, *counts;
+};
+struct ReleaseArgs {
+  const unsigned char* done;
+  int n_seqs;
+  int *lens, *n_free, *free_pages, *table;
+};
+struct RowsArgs {   // append: from k, v; read: to k, v
+  void *k, *v;
+  gsi_dtype_t dtype;
+  long long k_token, k_head, v_token, v_head;   // strides in elements
+  const int* slots;
+  int n;
+  unsigned char* pages;
+};
+struct AttendArgs {
+  const void* q;
+  void* out;
+  gsi_dtype_t dtype;
+  long long q_token, q_head, out_token, out_head;
+  int n_rows, n_q_heads, shared;   // shared: q heads of a head of the cache
+  float scale;
+  const int *q_start, *kv_len, *table;
+  int n_seqs;
+  const unsigned char* pages;
+  float* parts;        // what CTAs have of rows that they share
+  unsigned* tickets;   // [kMaxCtas]
+};
+
+cudaError_t launch_plan(const Shape& s, const PlanArgs& a, Control* ctl, cudaStream_t stream);
+cudaError_t launch_release(const Shape& s, const ReleaseArgs& a, Control* ctl, cudaStream_t stream);
+cudaError_t launch_append(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream);
+cudaError_t launch_read(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream);
+cudaError_t launch_attend(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream);
+
+__device__ __forceinline__ float load_as_float(const void* p, gsi_dtype_t t, long long i) {
+  if (t == GSI_F32) return static_cast<const float*>(p)[i];
+  if (t == GSI_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+  return __half2float(static_cast<const __half*>(p)[i]);
+}
+__device__ __forceinline__ void store_from_float(void* p, gsi_dtype_t t, long long i, float v) {
+  if (t == GSI_F32) static_cast<float*>(p)[i] = v;
+  else if (t == GSI_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+  else static_cast<__half*>(p)[i] = __float2half_rn(v);
+}
+
+}  // namespace kv
+}  // namespace gsi

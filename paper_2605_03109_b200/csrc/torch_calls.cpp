@@ -9,7 +9,11 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <climits>
+#include <memory>
+
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -21,6 +25,11 @@ namespace {
 decltype(&gsi_forward_n) forward_n = nullptr;
 decltype(&gsi_extend_basis) extend_basis = nullptr;
 decltype(&gsi_forward_static) forward_static = nullptr;
+decltype(&gsi_kv_plan) kv_plan = nullptr;
+decltype(&gsi_kv_release) kv_release = nullptr;
+decltype(&gsi_kv_append) kv_append = nullptr;
+decltype(&gsi_kv_read) kv_read = nullptr;
+decltype(&gsi_kv_attend) kv_attend = nullptr;
 
 struct NoGil {
   PyThreadState* state = PyEval_SaveThread();
@@ -195,8 +204,222 @@ PyObject* py_bind(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   Py_RETURN_NONE;
 }
 
+// ---- the cache of keys and values: a handle and the tensors of its state, in a capsule
+struct Cache {
+  gsi_kv_t handle = nullptr;
+  int64_t n_heads = 0, head_dim = 0, max_seqs = 0, layers = 0, n_seqs = 0;
+  at::Tensor pages, table, lens, free, n_free, q_start, kv_len, slots, positions, counts;
+  c10::Device device = c10::Device(c10::kCPU);
+};
+constexpr const char* kCacheName = "_torch_calls.cache";
+Cache* cache_of(PyObject* o) { return static_cast<Cache*>(PyCapsule_GetPointer(o, kCacheName)); }
+template <typename T>
+T* ptr(const at::Tensor& t) {
+  return static_cast<T*>(t.data_ptr());
+}
+bool refuse(const char* why) {
+  PyErr_SetString(PyExc_AssertionError, why);
+  return false;
+}
+bool type_of(const at::Tensor& t, gsi_dtype_t* out) {
+  switch (t.scalar_type()) {
+    case at::kFloat: *out = GSI_F32; return true;
+    case at::kBFloat16: *out = GSI_BF16; return true;
+    case at::kHalf: *out = GSI_F16; return true;
+    default: return refuse("float32, bfloat16 or float16 is expected");
+  }
+}
+// [n][heads][head_dim] on the cache's device, channels adjacent.
+bool rows_of(const Cache& c, const at::Tensor& t, int64_t heads, const char* what) {
+  if (t.device() == c.device && t.dim() == 3 && t.size(2) == c.head_dim && (heads == 0 || t.size(1) == heads) &&
+      (t.stride(2) == 1 || c.head_dim == 1) && t.size(0) <= INT_MAX)
+    return true;
+  return refuse(what);
+}
+bool ints_of(const Cache& c, const at::Tensor& t, at::ScalarType type) {
+  if (t.device() == c.device && t.scalar_type() == type && t.dim() == 1 && t.is_contiguous() && t.size(0) <= INT_MAX) return true;
+  return refuse(type == at::kInt ? "a contiguous vector of int32 on the cache's device is expected"
+                                 : "a contiguous vector of bool or uint8 on the cache's device is expected");
+}
+bool layer_of(const Cache& c, PyObject* o, void** pages) {
+  const int64_t layer = PyLong_AsLongLong(o);
+  if (PyErr_Occurred()) return false;
+  if (layer < 0 || layer >= c.layers) return refuse("no such layer");
+  *pages = ptr<char>(c.pages) + layer * (c.pages.numel() / c.layers);
+  return true;
+}
+gsi_stream_t stream_on(const Cache& c, bool given, void* stream) {
+  return static_cast<gsi_stream_t>(given ? stream : (void*)c10::cuda::getCurrentCUDAStream(c.device.index()).stream());
+}
+
+// kv_state(handle, n_heads, head_dim, layers, pages, table, lens, free, n_free, q_start, kv_len, slots, positions, counts) -> capsule
+PyObject* py_kv_state(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!enough(n_args, 14)) return nullptr;
+  auto c = std::make_unique<Cache>();
+  c->handle = static_cast<gsi_kv_t>(PyLong_AsVoidPtr(args[0]));
+  c->n_heads = PyLong_AsLongLong(args[1]);
+  c->head_dim = PyLong_AsLongLong(args[2]);
+  c->layers = PyLong_AsLongLong(args[3]);
+  if (PyErr_Occurred()) return nullptr;
+  at::Tensor* to[] = {&c->pages, &c->table, &c->lens, &c->free, &c->n_free, &c->q_start, &c->kv_len, &c->slots, &c->positions, &c->counts};
+  for (int i = 0; i < 10; ++i) {
+    const at::Tensor* t = tensor_of(args[4 + i]);
+    if (!t) return nullptr;
+    *to[i] = *t;
+  }
+  c->device = c->pages.device();
+  c->max_seqs = c->n_seqs = c->lens.numel();
+  return PyCapsule_New(c.release(), kCacheName, [](PyObject* o) { delete static_cast<Cache*>(PyCapsule_GetPointer(o, kCacheName)); });
+  END_HANDLE_TH_ERRORS
+}
+// kv_close(capsule): its handle is gone
+PyObject* py_kv_close(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  if (!enough(n_args, 1)) return nullptr;
+  Cache* c = cache_of(args[0]);
+  if (!c) return nullptr;
+  c->handle = nullptr;
+  Py_RETURN_NONE;
+}
+// kv_plan(capsule, n_new, commit, stream) -> status
+PyObject* py_kv_plan(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!enough(n_args, 4)) return nullptr;
+  Cache* c = cache_of(args[0]);
+  const at::Tensor* n_new = c ? tensor_of(args[1]) : nullptr;
+  const int commit = n_new ? PyObject_IsTrue(args[2]) : -1;
+  bool given;
+  void* stream;
+  if (commit < 0 || !ints_of(*c, *n_new, at::kInt) || !stream_of(args[3], &given, &stream)) return nullptr;
+  int status;
+  {
+    NoGil no_gil;
+    const c10::cuda::CUDAGuard guard(c->device);
+    status = kv_plan(c->handle, ptr<int>(*n_new), (int)n_new->numel(), commit, ptr<int>(c->lens), ptr<int>(c->n_free), ptr<int>(c->free),
+                     ptr<int>(c->table), ptr<int>(c->q_start), ptr<int>(c->kv_len), ptr<int>(c->slots), ptr<int>(c->positions),
+                     ptr<int>(c->counts), stream_on(*c, given, stream));
+  }
+  if (status == GSI_OK) c->n_seqs = n_new->numel();
+  return PyLong_FromLong(status);
+  END_HANDLE_TH_ERRORS
+}
+// kv_release(capsule, done, stream) -> status
+PyObject* py_kv_release(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!enough(n_args, 3)) return nullptr;
+  Cache* c = cache_of(args[0]);
+  const at::Tensor* done = c ? tensor_of(args[1]) : nullptr;
+  bool given;
+  void* stream;
+  if (!done || !ints_of(*c, *done, done->scalar_type() == at::kBool ? at::kBool : at::kByte) || !stream_of(args[2], &given, &stream)) return nullptr;
+  int status;
+  {
+    NoGil no_gil;
+    const c10::cuda::CUDAGuard guard(c->device);
+    status = kv_release(c->handle, ptr<unsigned char>(*done), (int)done->numel(), ptr<int>(c->lens), ptr<int>(c->n_free), ptr<int>(c->free),
+                        ptr<int>(c->table), stream_on(*c, given, stream));
+  }
+  return PyLong_FromLong(status);
+  END_HANDLE_TH_ERRORS
+}
+// kv_append(capsule, k, v, layer, slots or None, stream) -> status
+PyObject* py_kv_append(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!enough(n_args, 6)) return nullptr;
+  Cache* c = cache_of(args[0]);
+  const at::Tensor *k = c ? tensor_of(args[1]) : nullptr, *v = k ? tensor_of(args[2]) : nullptr;
+  const at::Tensor* slots = v ? (args[4] == Py_None ? &c->slots : tensor_of(args[4])) : nullptr;
+  bool given;
+  void *stream, *pages;
+  gsi_dtype_t type;
+  if (!slots || !rows_of(*c, *k, c->n_heads, "k must be [n][n_heads][head_dim] on the cache's device, channels adjacent") ||
+      !rows_of(*c, *v, c->n_heads, "v must be [n][n_heads][head_dim] on the cache's device, channels adjacent") || !type_of(*k, &type) ||
+      !ints_of(*c, *slots, at::kInt) || !layer_of(*c, args[3], &pages) || !stream_of(args[5], &given, &stream))
+    return nullptr;
+  if (k->scalar_type() != v->scalar_type() || k->size(0) != v->size(0)) return refuse("k and v differ in type or rows"), nullptr;
+  if (args[4] == Py_None ? slots->numel() < k->size(0) : slots->numel() != k->size(0)) return refuse("a slot for each row is expected"), nullptr;
+  int status;
+  {
+    NoGil no_gil;
+    const c10::cuda::CUDAGuard guard(c->device);
+    status = kv_append(c->handle, k->data_ptr(), v->data_ptr(), type, k->stride(0), k->stride(1), v->stride(0), v->stride(1), ptr<int>(*slots),
+                       (int)k->size(0), pages, stream_on(*c, given, stream));
+  }
+  return PyLong_FromLong(status);
+  END_HANDLE_TH_ERRORS
+}
+// kv_read(capsule, slots, layer, like (a tensor of the type that is wanted), stream) -> (status, k, v)
+PyObject* py_kv_read(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!enough(n_args, 5)) return nullptr;
+  Cache* c = cache_of(args[0]);
+  const at::Tensor *slots = c ? tensor_of(args[1]) : nullptr, *like = slots ? tensor_of(args[3]) : nullptr;
+  bool given;
+  void *stream, *pages;
+  gsi_dtype_t type;
+  if (!like || !type_of(*like, &type) || !ints_of(*c, *slots, at::kInt) || !layer_of(*c, args[2], &pages) || !stream_of(args[4], &given, &stream))
+    return nullptr;
+  at::Tensor k, v;
+  int status;
+  {
+    NoGil no_gil;
+    const c10::cuda::CUDAGuard guard(c->device);
+    const auto options = slots->options().dtype(like->scalar_type());
+    k = at::empty({slots->numel(), c->n_heads, c->head_dim}, options);
+    v = at::empty({slots->numel(), c->n_heads, c->head_dim}, options);
+    status = kv_read(c->handle, pages, ptr<int>(*slots), (int)slots->numel(), type, k.data_ptr(), v.data_ptr(), stream_on(*c, given, stream));
+  }
+  return Py_BuildValue("iNN", status, THPVariable_Wrap(k), THPVariable_Wrap(v));
+  END_HANDLE_TH_ERRORS
+}
+// kv_attend(capsule, q, layer, scale, out or None, stream) -> (status, out)
+PyObject* py_kv_attend(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!enough(n_args, 6)) return nullptr;
+  Cache* c = cache_of(args[0]);
+  const at::Tensor* q = c ? tensor_of(args[1]) : nullptr;
+  const double scale = q ? PyFloat_AsDouble(args[3]) : 0.0;
+  if (PyErr_Occurred()) return nullptr;
+  bool given;
+  void *stream, *pages;
+  gsi_dtype_t type;
+  at::Tensor out;
+  if (!q || !rows_of(*c, *q, 0, "q must be [n][heads][head_dim] on the cache's device, channels adjacent") || !type_of(*q, &type) ||
+      !layer_of(*c, args[2], &pages) || !output_of(args[4], &out) || !stream_of(args[5], &given, &stream))
+    return nullptr;
+  if (q->size(1) < 1 || q->size(1) > INT_MAX || q->size(1) % c->n_heads) return refuse("the heads of q must be a multiple of the cache's"), nullptr;
+  if (out.defined()) {
+    if (!rows_of(*c, out, q->size(1), "out must be of q's shape, on its device, channels adjacent")) return nullptr;
+    if (out.size(0) != q->size(0) || out.scalar_type() != q->scalar_type()) return refuse("out must be of q's shape and type"), nullptr;
+  }
+  int status;
+  {
+    NoGil no_gil;
+    const c10::cuda::CUDAGuard guard(c->device);
+    if (!out.defined()) out = at::empty({q->size(0), q->size(1), q->size(2)}, q->options());
+    status = kv_attend(c->handle, q->data_ptr(), type, q->stride(0), q->stride(1), (int)q->size(0), (int)q->size(1), (float)scale,
+                       ptr<int>(c->q_start), ptr<int>(c->kv_len), ptr<int>(c->table), (int)c->n_seqs, pages, out.data_ptr(), out.stride(0),
+                       out.stride(1), stream_on(*c, given, stream));
+  }
+  return Py_BuildValue("iN", status, THPVariable_Wrap(out));
+  END_HANDLE_TH_ERRORS
+}
+// bind_kv(addresses of gsi_kv_plan, _release, _append, _read, _attend)
+PyObject* py_bind_kv(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  if (!enough(n_args, 5)) return nullptr;
+  kv_plan = reinterpret_cast<decltype(kv_plan)>(PyLong_AsVoidPtr(args[0]));
+  kv_release = reinterpret_cast<decltype(kv_release)>(PyLong_AsVoidPtr(args[1]));
+  kv_append = reinterpret_cast<decltype(kv_append)>(PyLong_AsVoidPtr(args[2]));
+  kv_read = reinterpret_cast<decltype(kv_read)>(PyLong_AsVoidPtr(args[3]));
+  kv_attend = reinterpret_cast<decltype(kv_attend)>(PyLong_AsVoidPtr(args[4]));
+  if (PyErr_Occurred()) return nullptr;
+  Py_RETURN_NONE;
+}
+
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {METHOD(forward), METHOD(extend), METHOD(forward_static), METHOD(bind), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {METHOD(forward), METHOD(extend), METHOD(forward_static), METHOD(bind),
+                         METHOD(kv_state), METHOD(kv_close), METHOD(kv_plan), METHOD(kv_release), METHOD(kv_append), METHOD(kv_read),
+                         METHOD(kv_attend), METHOD(bind_kv), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods};
 
 }  // namespace
