@@ -17,37 +17,6 @@ constexpr int kPlanGrid = 296;
 __device__ __forceinline__ int clamp_int(long long v) { return v > 0x7fffffffll ? 0x7fffffff : (int)v; }
 __device__ __forceinline__ int pages_of(long long tokens, int page_tokens) { return (int)((tokens + page_tokens - 1) / page_tokens); }
 
-// Sums over the block of two values per thread: exclusive prefixes (in thread order) and totals.
-struct Scan2 {
-  long long a, b;
-};
-__device__ __forceinline__ Scan2 block_scan(Scan2 v, Scan2* total, Scan2* s_warp) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  Scan2 x = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long a = __shfl_up_sync(0xffffffffu, x.a, o), b = __shfl_up_sync(0xffffffffu, x.b, o);
-    if (lane >= o) {
-      x.a += a;
-      x.b += b;
-    }
-  }
-  if (lane == 31) s_warp[warp] = x;
-  __syncthreads();
-  Scan2 before{0, 0}, all{0, 0};
-  for (int w = 0; w < warps; ++w) {
-    if (w < warp) {
-      before.a += s_warp[w].a;
-      before.b += s_warp[w].b;
-    }
-    all.a += s_warp[w].a;
-    all.b += s_warp[w].b;
-  }
-  __syncthreads();
-  *total = all;
-  return {before.a + x.a - v.a, before.b + x.b - v.b};
-}
-
 // The last index s with first[s] <= i (first[0] <= i, ascending).
 __device__ __forceinline__ int last_at_most(const int* first, int n, int i) {
   int lo = 0, hi = n;   // first[lo] <= i < first[hi]
@@ -522,7 +491,7 @@ gsi_status_t gsi_kv_create(const gsi_kv_desc_t* desc, void* workspace, size_t wo
   h->tickets = reinterpret_cast<unsigned*>(ws + up256(sizeof(kv::Control)));
   h->parts = reinterpret_cast<float*>(ws + up256(sizeof(kv::Control)) + up256(kv::kMaxCtas * 4));
   h->last_stream = stream;
-  if (cudaGetDevice(&h->device) != cudaSuccess ||
+  if (cudaGetDevice(&h->device) != cudaSuccess || kv::prepare_attend(s) != cudaSuccess ||
       cudaMemsetAsync(ws, 0, up256(sizeof(kv::Control)) + up256(kv::kMaxCtas * 4), stream) != cudaSuccess ||
       cudaStreamSynchronize(stream) != cudaSuccess) {
     delete h;
@@ -587,7 +556,7 @@ gsi_status_t gsi_kv_attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t
   if (!h || !is_type(dtype) || n_rows < 0 || n_q_heads <= 0 || n_q_heads % h->shape.n_heads || n_seqs <= 0 || n_seqs > h->shape.max_seqs ||
       !std::isfinite(scale))
     return GSI_ERR_INVALID_ARG;
-  if (n_q_heads > 1 << 20) return GSI_ERR_UNSUPPORTED;
+  if ((long long)n_rows * (n_q_heads / h->shape.n_heads) >= 1ll << 31) return GSI_ERR_UNSUPPORTED;
   if (n_rows == 0) return GSI_OK;
   if (!aligned(q, size_of(dtype)) || !aligned(out, size_of(dtype)) || !aligned(pages, 16)) return GSI_ERR_INVALID_ARG;
   for (const int* p : {q_start, kv_len, table})

@@ -78,7 +78,39 @@ cudaError_t launch_plan(const Shape& s, const PlanArgs& a, Control* ctl, cudaStr
 cudaError_t launch_release(const Shape& s, const ReleaseArgs& a, Control* ctl, cudaStream_t stream);
 cudaError_t launch_append(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream);
 cudaError_t launch_read(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream);
+cudaError_t prepare_attend(const Shape& s);   // once for a handle, on its device
 cudaError_t launch_attend(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream);
+
+// Sums over the block of two values per thread: exclusive prefixes (in thread order) and totals.
+struct Scan2 {
+  long long a, b;
+};
+__device__ __forceinline__ Scan2 block_scan(Scan2 v, Scan2* total, Scan2* s_warp) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  Scan2 x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long a = __shfl_up_sync(0xffffffffu, x.a, o), b = __shfl_up_sync(0xffffffffu, x.b, o);
+    if (lane >= o) {
+      x.a += a;
+      x.b += b;
+    }
+  }
+  if (lane == 31) s_warp[warp] = x;
+  __syncthreads();
+  Scan2 before{0, 0}, all{0, 0};
+  for (int w = 0; w < warps; ++w) {
+    if (w < warp) {
+      before.a += s_warp[w].a;
+      before.b += s_warp[w].b;
+    }
+    all.a += s_warp[w].a;
+    all.b += s_warp[w].b;
+  }
+  __syncthreads();
+  *total = all;
+  return {before.a + x.a - v.a, before.b + x.b - v.b};
+}
 
 __device__ __forceinline__ float load_as_float(const void* p, gsi_dtype_t t, long long i) {
   if (t == GSI_F32) return static_cast<const float*>(p)[i];
