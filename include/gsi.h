@@ -542,7 +542,8 @@ gsi_status_t gsi_kv_read(gsi_kv_t h, const void* pages, const int* slots, int n,
  * q, out: n_rows rows of n_q_heads x head_dim of `dtype`, n_q_heads a multiple of n_heads: q head j goes with
  * head j / (n_q_heads / n_heads).  Strides in elements, channels adjacent, >= 0 (out's rows apart from each
  * other).  Rows behind the last sequence's are left as they were.  Softmax and sums are held in fp32; the contractions
- * take q and the probabilities rounded to 22 bits for fp32, to 11 for 16-bit types.  A page number outside the
+ * take an fp32 q to 2^-24 of its row's largest channel and the probabilities in 22 bits, a 16-bit q as it is and the
+ * probabilities in 11 bits.  A page number outside the
  * pool, or a length outside the table, is reported by the status word (GSI_ERR_INVALID_ARG) and gives
  * NaN in the rows that would see it.  Which sums are made where follows from the lengths; a call is reproducible
  * bit for bit.
@@ -552,7 +553,8 @@ gsi_status_t gsi_kv_attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t
                            const int* kv_len, const int* table, int n_seqs, const void* pages, void* out,
                            int64_t out_token_stride, int64_t out_head_stride, gsi_stream_t stream);
 
-/* Synchronises the handle's last stream and returns the status word, which stays set. */
+/* Synchronises the handle's last stream and returns the status word, which stays set.  After GSI_ERR_TIMEOUT (a copy within
+ * the GPU did not arrive for seconds) the outputs of that call are undefined and the handle has to be made again. */
 gsi_status_t gsi_kv_get_status(gsi_kv_t h, int* device_status);
 gsi_status_t gsi_kv_destroy(gsi_kv_t h);
 

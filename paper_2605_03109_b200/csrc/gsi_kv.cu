@@ -409,7 +409,7 @@ struct gsi_kv {
 namespace {
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
-size_t parts_bytes(const kv::Shape& s) { return (size_t)kv::kMaxCtas * 2 * kv::kMaxRows * (s.groups * kv::kGroup + 2) * 4; }
+size_t parts_bytes(const kv::Shape& s) { return (size_t)kv::kMaxShares * 2 * kv::kPartFloats(s.groups) * 4; }
 
 gsi_status_t make_shape(const gsi_kv_desc_t* d, kv::Shape* s) {
   if (!d) return GSI_ERR_INVALID_ARG;
@@ -457,7 +457,7 @@ size_t gsi_kv_page_bytes(const gsi_kv_desc_t* desc) {
 
 size_t gsi_kv_workspace_bytes(const gsi_kv_desc_t* desc) {
   kv::Shape s;
-  return make_shape(desc, &s) == GSI_OK ? up256(sizeof(kv::Control)) + up256(kv::kMaxCtas * 4) + up256(parts_bytes(s)) : 0;
+  return make_shape(desc, &s) == GSI_OK ? up256(sizeof(kv::Control)) + up256(kv::kMaxShares * 4) + up256(parts_bytes(s)) : 0;
 }
 
 gsi_status_t gsi_kv_locate(const gsi_kv_desc_t* desc, int slot, int head, int channel, int is_v, size_t* code_byte_out,
@@ -489,10 +489,10 @@ gsi_status_t gsi_kv_create(const gsi_kv_desc_t* desc, void* workspace, size_t wo
   h->shape = s;
   h->ctl = reinterpret_cast<kv::Control*>(ws);
   h->tickets = reinterpret_cast<unsigned*>(ws + up256(sizeof(kv::Control)));
-  h->parts = reinterpret_cast<float*>(ws + up256(sizeof(kv::Control)) + up256(kv::kMaxCtas * 4));
+  h->parts = reinterpret_cast<float*>(ws + up256(sizeof(kv::Control)) + up256(kv::kMaxShares * 4));
   h->last_stream = stream;
   if (cudaGetDevice(&h->device) != cudaSuccess || kv::prepare_attend(s) != cudaSuccess ||
-      cudaMemsetAsync(ws, 0, up256(sizeof(kv::Control)) + up256(kv::kMaxCtas * 4), stream) != cudaSuccess ||
+      cudaMemsetAsync(ws, 0, up256(sizeof(kv::Control)) + up256(kv::kMaxShares * 4), stream) != cudaSuccess ||
       cudaStreamSynchronize(stream) != cudaSuccess) {
     delete h;
     return GSI_ERR_CUDA;

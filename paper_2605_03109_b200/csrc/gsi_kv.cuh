@@ -12,8 +12,10 @@ constexpr int kTile = 16;          // tokens of a tile
 constexpr int kGroup = 64;         // channels that share a pair (s, mid)
 constexpr int kCodeBytes = 512;    // codes of a block: 16 tokens x 64 channels, 16 bytes a lane of a warp
 constexpr int kBlockBytes = 576;   // ... and 16 pairs
-constexpr int kMaxCtas = 320;      // of the attention's grid: what the workspace has room for
-constexpr int kMaxRows = 16;       // rows of the attention that a CTA takes at a time
+constexpr int kMaxShares = 296 * 8;   // warps of the attention's grid
+constexpr int kMaxRows = 16;          // rows of the attention that a warp takes at a time
+// What a warp leaves of rows that it shares with others, for heads of that many blocks.
+constexpr int kPartFloats(int groups) { return (groups <= 2 ? kMaxRows : kMaxRows / 2) * (groups * kGroup + 8); }
 
 // Layout within a block, of token t (0..15) and channel c (0..63).  K is the A operand of m16n8k16 with tokens as
 // its rows: lane 4 (t % 8) + c / 16 holds 16 channels of tokens t % 8 and t % 8 + 8.  V is the A operand with
@@ -70,8 +72,8 @@ struct AttendArgs {
   const int *q_start, *kv_len, *table;
   int n_seqs;
   const unsigned char* pages;
-  float* parts;        // what CTAs have of rows that they share
-  unsigned* tickets;   // [kMaxCtas]
+  float* parts;        // [kMaxShares][2]: what a warp has of a segment begun before its share, and of one that ends behind it
+  unsigned* tickets;   // [kMaxShares]
 };
 
 cudaError_t launch_plan(const Shape& s, const PlanArgs& a, Control* ctl, cudaStream_t stream);

@@ -13,9 +13,11 @@
 //
 // Codes of K enter as f16 subnormals, code 2^-24 (a mask, exact; the channels in the upper half of a byte as 16 code,
 // against q / 16).  Those of V enter as code - 8 (mask, one f16 instruction, exact): sums of random signs,
-// where sums of codes would cancel against the mid part.  fp32 rows take two columns each, the two f16 terms of q 2^k
-// (|q 2^k| < 2^14) and of p s: 22 bits; 16-bit rows take one: q exact, p s in 11 bits.  The tensor cores truncate as
-// they add, so fp32 rows hand their sums over to fp32 additions every kFlush tiles.
+// where sums of codes would cancel against the mid part.  fp32 rows take two columns each.  Those of q are whole numbers, q 2^k
+// = hi + lo / 4096 with |hi|, |lo| <= 2^11 (so q is held to 2^-24 of its row's largest): a block's sums of codes times
+// whole numbers stay below 2^21, and the tensor cores, which truncate as they add, add them exactly (with two f16 terms instead the
+// scores were three times as far off).  Those of p s are two f16 terms, 22 bits; their sums are handed over to
+// fp32 additions every kFlush tiles.  16-bit rows take one column: q exact, p s in 11 bits.
 #include <type_traits>
 
 #include "gsi_kv.cuh"
@@ -34,36 +36,34 @@ using umma::s32;
 
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
-constexpr int kGrid = 296;       // two blocks an SM
-constexpr int kFlush = 16;      // tiles between sums in fp32 (T = 2)
-constexpr int kSnap = 8;        // tiles: the share of a CTA ends with a segment that ends as near
-constexpr int kMostShares = 64; // CTAs that share a segment
+constexpr int kGrid = kMaxShares / kWarps;   // two blocks an SM
+constexpr int kFlush = 32;      // tiles between sums in fp32 (T = 2)
+constexpr int kSnap = 4;        // tiles: the share of a warp ends with a segment that ends as near
+constexpr float kLow = 4096.f;  // units of the second term of q in one of the first
 constexpr float kLazy = 8.f;    // a running maximum is left where it is while 2^score stays below 2^kLazy above it
 constexpr float kOne = 64.f;    // p s <= 2^kLazy kOne s / vs < 2^15
+constexpr float kNone = -3e38f; // the maximum of no score
 
 // G: blocks of 64 channels; T: f16 terms of an operand; NT: column tiles of eight
 template <int G, int T, int NT>
 struct Cfg {
   static constexpr int kDim = G * kGroup;
-  static constexpr int kRows = NT * 8 / T;   // rows of a CTA
+  static constexpr int kRows = NT * 8 / T;           // rows of a warp
   static constexpr int kLaneRows = T == 1 ? 2 : 1;   // ... of a lane per column tile
   static constexpr int kTileBytes = G * 2 * kBlockBytes;
-  static constexpr int kStages = G == 1 ? 6 : G == 2 ? 4 : 2;
-  static constexpr int kAreaStride = kDim + 8;
-  static constexpr int kAreaRows = T == 2 ? NT * 4 : 4;   // rows of a warp that are summed at a time
-  static constexpr int kRing = kWarps * kStages * kTileBytes;
+  static constexpr int kStages = G == 1 ? 8 : G == 2 ? 4 : 2;
+  static constexpr int kPair = G * NT <= 2 ? 2 : 1;  // tiles in one pass, where registers have room
+  static constexpr int kRing = kStages * kTileBytes;
   static constexpr int kQ = NT * G * 1024;
-  static constexpr int kArea = kWarps * kAreaRows * kAreaStride * 4;
-  static constexpr int kSums = (G + 1) * kMaxRows * 4;          // sums of q by block, factors of the scores
-  static constexpr int kMl = 2 * kWarps * kMaxRows * 4;         // maxima and sums of the warps
-  static constexpr int kBars = kWarps * kStages * 8;
-  static constexpr int kSmem = kRing + kQ + kArea + kSums + kMl + kBars;
-  static constexpr int kPart = kMaxRows * (kDim + 2);           // floats of a part
+  static constexpr int kSums = (3 * G + 1) * kRows * 4;   // per block: the sum of q and -8 times its terms'; factors of the scores
+  static constexpr int kBars = kStages * 8;
+  static constexpr int kWarpBytes = (kRing + kQ + kSums + kBars + 15) / 16 * 16;
+  static constexpr int kSmem = kWarps * kWarpBytes;
+  static constexpr int kPart = kRows * (kDim + 8);   // floats of a part: sums, then (maximum, sum of p) of the rows
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -76,16 +76,6 @@ __device__ __forceinline__ float exp2_fast(float v) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-  return v;
 }
 __device__ __forceinline__ float2 unpack_half2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
@@ -127,414 +117,484 @@ __device__ __forceinline__ Seq load_seq(const Shape& s, const AttendArgs& a, int
   return q;
 }
 
+// A segment that warps share, whose last warp is of this block.
+struct Pending {
+  int first, parts, rows;
+  long long out[kMaxRows];
+};
+
 template <int G, int T, int NT>
 __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a, Control* ctl) {
   using C = Cfg<G, T, NT>;
   constexpr int kLR = C::kLaneRows;
   extern __shared__ __align__(128) unsigned char smem[];
-  unsigned char* s_q = smem + C::kRing;
-  float* s_area = reinterpret_cast<float*>(s_q + C::kQ);
-  float* s_sum = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(s_area) + C::kArea);   // [G][kMaxRows]
-  float* s_factor = s_sum + G * kMaxRows;
-  float* s_m = s_factor + kMaxRows;                // [kWarps][kMaxRows]
-  float* s_l = s_m + kWarps * kMaxRows;
-  uint64_t* s_bar = reinterpret_cast<uint64_t*>(s_l + kWarps * kMaxRows);
   __shared__ Scan2 s_warp[kWarps];
-  __shared__ long long s_at[2], s_base[2];   // the CTA's first unit and the one behind its last; the first unit of its first sequence
-  __shared__ int s_seq, s_last;
+  __shared__ long long s_before[kThreads];   // units before a thread's sequences
+  __shared__ Pending s_pending[kWarps * 2];
+  __shared__ int s_n_pending;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gr = lane >> 2, t4 = lane & 3;
+  unsigned char* ring = smem + warp * C::kWarpBytes;
+  unsigned char* s_q = ring + C::kRing;
+  float* s_sum = reinterpret_cast<float*>(s_q + C::kQ);   // [G][kRows]
+  float* s_start = s_sum + G * C::kRows;                  // [G][kRows][2]
+  float* s_factor = s_start + 2 * G * C::kRows;           // [kRows]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(s_factor + C::kRows);
 
   if (lane == 0)
-    for (int i = 0; i < C::kStages; ++i) mbar_init(s_bar + warp * C::kStages + i, 1);
+    for (int i = 0; i < C::kStages; ++i) mbar_init(bars + i, 1);
+  for (int i = lane; i < (C::kQ + C::kSums) / 4; i += 32) reinterpret_cast<uint32_t*>(s_q)[i] = 0u;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  if (tid == 0) s_n_pending = 0;
 
   // ---- shares: the units of all sequences in order, in even pieces that end with a segment where one ends near
-  const int per = (a.n_seqs + kThreads - 1) / kThreads, first = tid * per, last = min(first + per, a.n_seqs);
+  const int per = (a.n_seqs + kThreads - 1) / kThreads;
   Scan2 sum{0, 0}, total;
-  for (int i = first; i < last; ++i) {
-    const Seq q = load_seq<C::kRows>(s, a, i);
-    sum.a += q.segments(s) * q.tiles;
-    sum.b += q.segments(s);
+  for (int i = tid * per; i < min(tid * per + per, a.n_seqs); ++i) {
+    const Seq x = load_seq<C::kRows>(s, a, i);
+    sum.a += x.segments(s) * x.tiles;
+    sum.b += x.segments(s);
   }
-  const Scan2 before = block_scan(sum, &total, s_warp);
-  if (total.a == 0) return;
-  const long long shares = max(1ll, min(min((long long)gridDim.x, max(total.a / kWarps, total.b)), total.b * kMostShares));
-  const int b = blockIdx.x;
-  if (b >= shares) return;
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const long long x = total.a * (b + e) / shares;
-    if (x >= total.a) {
-      if (tid == 0) s_at[e] = total.a;
-    } else if (x >= before.a && x < before.a + sum.a) {
-      long long base = before.a;
-      int i = first;
-      Seq q = load_seq<C::kRows>(s, a, i);
-      for (long long n; x >= base + (n = q.segments(s) * q.tiles);) {
-        base += n;
-        q = load_seq<C::kRows>(s, a, ++i);
-      }
-      const long long begin = base + (x - base) / q.tiles * q.tiles, from = x - begin, to = begin + q.tiles - x;
-      s_at[e] = from < kSnap && from <= to ? begin : to < kSnap ? begin + q.tiles : x;
-      if (e == 0) {
-        s_base[0] = base;
-        s_seq = i;
-      }
-    }
-  }
+  s_before[tid] = block_scan(sum, &total, s_warp).a;
+  const long long shares = max(1ll, min((long long)kMaxShares, max(total.a / kSnap, total.b)));
+  const int share = warp * kGrid + blockIdx.x;   // (few shares: one a block)
+  const bool any = total.a > 0 && share < shares;
+  if (total.a == 0 || blockIdx.x >= shares) return;
   __syncthreads();
-  const long long u0 = s_at[0], u1 = s_at[1];
-  if (u0 >= u1) return;
-  int seq = s_seq;
-  long long base = s_base[0];
-  Seq q = load_seq<C::kRows>(s, a, seq);
-  while (u0 >= base + q.segments(s) * q.tiles) {   // (the share begins where the sequence ended)
-    base += q.segments(s) * q.tiles;
-    q = load_seq<C::kRows>(s, a, ++seq);
-  }
-
-  // ---- the warp's tiles: units u0 + warp + 8 j, through a ring of its own; lane j % 32 knows where tile j lies
-  const uint32_t ring = s32(smem) + warp * C::kStages * C::kTileBytes;
-  uint64_t* bars = s_bar + warp * C::kStages;
-  const int mine = u1 - u0 > warp ? (int)((u1 - u0 - warp + kWarps - 1) / kWarps) : 0;   // its tiles
-  int look_seq = seq;
-  long long look_base = base;
-  const unsigned char* where = nullptr;
-  unsigned bad[2] = {0u, 0u};
-  auto look_up = [&](int batch) {
-    const long long u = u0 + warp + (long long)kWarps * (batch * 32 + lane);
-    bool wrong = false;
-    where = nullptr;
-    if (u < u1) {
-      Seq x = load_seq<C::kRows>(s, a, look_seq);
-      for (long long n; u >= look_base + (n = x.segments(s) * x.tiles);) {
-        look_base += n;
-        x = load_seq<C::kRows>(s, a, ++look_seq);
-      }
-      const long long local = u - look_base, segment = local / x.tiles;
-      const int tile = (int)(local - segment * x.tiles), head = (int)(segment / x.n_row_tiles);
-      if ((long long)tile * kTile < x.len) {
-        const int index = tile / s.page_tiles;
-        const int page = index < s.max_pages ? __ldg(a.table + (long long)look_seq * s.max_pages + index) : -1;
-        wrong = (unsigned)page >= (unsigned)s.n_pages;
-        if (!wrong) where = a.pages + tile_at(s, page, head, tile - index * s.page_tiles);
-      }
+  // where a share begins: the unit, its sequence and that one's first unit
+  auto begin_of = [&](int x_share, int* x_seq, long long* x_base) {
+    const long long x = total.a * x_share / shares;
+    if (x >= total.a) return total.a;
+    int lo = 0, hi = kThreads;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (s_before[mid] <= x) lo = mid;
+      else hi = mid;
     }
-    bad[batch & 1] = __ballot_sync(0xffffffffu, wrong);
+    long long base = s_before[lo];
+    int i = lo * per;
+    Seq q = load_seq<C::kRows>(s, a, i);
+    for (long long n; x >= base + (n = q.segments(s) * q.tiles);) {
+      base += n;
+      q = load_seq<C::kRows>(s, a, ++i);
+    }
+    *x_seq = i;
+    *x_base = base;
+    const long long begin = base + (x - base) / q.tiles * q.tiles, from = x - begin, to = begin + q.tiles - x;
+    return from < kSnap && from <= to ? begin : to < kSnap ? begin + q.tiles : x;
   };
-  int issued = 0;
-  auto issue = [&]() {
-    if (issued >= mine) return;
-    if ((issued & 31) == 0) look_up(issued >> 5);
-    if (lane == (issued & 31)) {
-      uint64_t* bar = bars + issued % C::kStages;
-      if (where) {
-        mbar_expect_tx(bar, C::kTileBytes);
-        copy_tile(ring + (issued % C::kStages) * C::kTileBytes, where, C::kTileBytes, bar);
-      } else {
-        mbar_arrive(bar);
+
+  if (any) {
+    int seq = 0;
+    long long base = 0, skip_base;
+    int skip_seq;
+    const long long u0 = begin_of(share, &seq, &base), u1 = begin_of(share + 1, &skip_seq, &skip_base);
+    const int mine = (int)(u1 - u0);   // the warp's tiles
+    Seq q;
+    int head = 0, row_tile = 0, tile = 0;   // of the next unit
+    if (mine > 0) {
+      q = load_seq<C::kRows>(s, a, seq);
+      while (u0 >= base + q.segments(s) * q.tiles) {   // (the share begins where the sequence ended)
+        base += q.segments(s) * q.tiles;
+        q = load_seq<C::kRows>(s, a, ++seq);
       }
+      const long long segment = (u0 - base) / q.tiles;
+      tile = (int)(u0 - base - segment * q.tiles);
+      head = (int)(segment / q.n_row_tiles);
+      row_tile = (int)(segment - (long long)head * q.n_row_tiles);
     }
-    ++issued;
-    __syncwarp();
-  };
-  for (int i = 0; i < C::kStages; ++i) issue();
 
-  int j = 0;         // the warp's next tile
-  bool gave_up = false;    // a copy did not arrive
+    // ---- its tiles come through a ring; lane j % 32 knows where tile j lies
+    int look_seq = seq;
+    long long look_base = base;
+    const unsigned char* where = nullptr;
+    unsigned bad_even = 0u, bad_odd = 0u;   // tiles without a page, of batches of 32
+    auto look_up = [&](int batch) {
+      const long long u = u0 + batch * 32 + lane;
+      bool wrong = false;
+      where = nullptr;
+      if (u < u1) {
+        Seq x = load_seq<C::kRows>(s, a, look_seq);
+        for (long long n; u >= look_base + (n = x.segments(s) * x.tiles);) {
+          look_base += n;
+          x = load_seq<C::kRows>(s, a, ++look_seq);
+        }
+        const long long local = u - look_base;
+        int at, of;
+        if (local >> 31) {
+          const long long segment = local / x.tiles;
+          at = (int)(local - segment * x.tiles);
+          of = (int)(segment / x.n_row_tiles);
+        } else {
+          const unsigned segment = (unsigned)local / (unsigned)x.tiles;
+          at = (int)((unsigned)local - segment * (unsigned)x.tiles);
+          of = (int)(segment / (unsigned)x.n_row_tiles);
+        }
+        if ((long long)at * kTile < x.len) {
+          const int index = at / s.page_tiles;
+          const int page = index < s.max_pages ? __ldg(a.table + (long long)look_seq * s.max_pages + index) : -1;
+          wrong = (unsigned)page >= (unsigned)s.n_pages;
+          if (!wrong) where = a.pages + tile_at(s, page, of, at - index * s.page_tiles);
+        }
+      }
+      const unsigned mask = __ballot_sync(0xffffffffu, wrong);
+      if (batch & 1) bad_odd = mask;
+      else bad_even = mask;
+    };
+    int issued = 0, to_stage = 0;
+    auto issue = [&]() {
+      if (issued >= mine) return;
+      if ((issued & 31) == 0) look_up(issued >> 5);
+      if (lane == (issued & 31)) {
+        if (where) {
+          mbar_expect_tx(bars + to_stage, C::kTileBytes);
+          copy_tile(s32(ring) + to_stage * C::kTileBytes, where, C::kTileBytes, bars + to_stage);
+        } else {
+          mbar_arrive(bars + to_stage);
+        }
+      }
+      ++issued;
+      if (++to_stage == C::kStages) to_stage = 0;
+    };
+    for (int i = 0; i < C::kStages; ++i) issue();
 
-  // ---- segments of the share
-  for (long long u = u0; u < u1;) {
-    while (u >= base + q.segments(s) * q.tiles) {
-      base += q.segments(s) * q.tiles;
-      q = load_seq<C::kRows>(s, a, ++seq);
-    }
-    const long long segment = (u - base) / q.tiles, begin = base + segment * q.tiles, end = begin + q.tiles, upto = min(end, u1);
-    const int head = (int)(segment / q.n_row_tiles), row0 = (int)(segment - (long long)head * q.n_row_tiles) * C::kRows;
-    const int n_rows = min(C::kRows, q.m * a.shared - row0);
-    // row r of the tile: row i of the step, q head
-    auto step_row = [&](int r) { return (row0 + r) / a.shared; };
-    auto q_head = [&](int r) { return head * a.shared + (row0 + r) % a.shared; };
-    auto sees = [&](int r) { return q.seen + step_row(min(r, n_rows - 1)) + 1; };
+    int stage = 0;
+    uint32_t phase = 0;
+    bool gave_up = false;    // a copy did not arrive
+    auto arrived = [&]() {   // the next tile; its place
+      if (__any_sync(0xffffffffu, !mbar_wait(bars + stage, phase))) gave_up = true;
+      const unsigned char* at = ring + stage * C::kTileBytes;
+      if (++stage == C::kStages) {
+        stage = 0;
+        phase ^= 1u;
+      }
+      return at;
+    };
 
-    // the rows as B operand: a warp takes a row, a lane 2 G channels
-    for (int r = warp; r < C::kRows; r += kWarps) {
-      float v[2 * G], top = 0.f;
-#pragma unroll
-      for (int i = 0; i < 2 * G; ++i) {
-        const int c = i * 32 + lane;
-        v[i] = r < n_rows && c < s.head_dim
-                   ? load_as_float(a.q, a.dtype, (q.q0 + step_row(r)) * a.q_token + q_head(r) * a.q_head + c) : 0.f;
-        top = fmaxf(top, fabsf(v[i]));
-      }
-#pragma unroll
-      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      int k = 0;
-      if (top > 0.f && top <= 3.402823466e38f) {
-        int e;
-        frexpf(top, &e);
-        k = 14 - e;
-      }
-      float part[G];
-#pragma unroll
-      for (int g = 0; g < G; ++g) part[g] = 0.f;
-#pragma unroll
-      for (int i = 0; i < 2 * G; ++i) {
-        const int c = (i & 1) * 32 + lane, g = i >> 1, nib = c & 7;   // channel of the block, of its word
-        const float x = scalbnf(v[i], k);
-        part[g] += x;
-        const float y = (nib & 1) ? x * 0.0625f : x;
-        const __half hi = __float2half_rn(y);
-        // word (c % 16) / 8 of lane c / 16: its two steps' registers (nib / 2) % 2, b0 or b1 nib % 2, half nib / 4
-        const int col = T == 2 ? (r & 3) * 2 : r & 7, nt = T == 2 ? r >> 2 : r >> 3;
-        __half* to = reinterpret_cast<__half*>(s_q + ((nt * G + g) * 2 + (c % 16) / 8) * 512 + (col * 4 + c / 16) * 16) + (nib / 2 % 2) * 4 +
-                     (nib & 1) * 2 + nib / 4;
-        *to = hi;
-        if constexpr (T == 2) to[32] = __float2half_rn(y - __half2float(hi));   // the next column: 4 lanes of 16 bytes on
-      }
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        part[g] = warp_sum(part[g]);
-        if (lane == 0) s_sum[g * kMaxRows + r] = part[g] * 0x1p-24f;
-      }
-      if (lane == 0) s_factor[r] = (float)fmin(ldexp((double)a.scale * 1.4426950408889634, 24 - k), 0x1p100);
-    }
-    __syncthreads();
+    // ---- segments of the share
+    for (int j = 0; j < mine && !gave_up;) {
+      const int n_tiles = min(q.tiles - tile, mine - j);   // of this segment
+      const int row0 = row_tile * C::kRows, n_rows = min(C::kRows, q.m * a.shared - row0);
+      // row r of the tile: row of the step, q head; its tokens
+      auto step_row = [&](int r) { return (row0 + r) / a.shared; };
+      auto q_head = [&](int r) { return head * a.shared + (row0 + r) % a.shared; };
+      auto sees = [&](int r) { return q.seen + step_row(min(r, n_rows - 1)) + 1; };
 
-    float O[NT][G][4][4], z[NT][kLR][G], m[NT][kLR], l[NT][kLR], m_flush[NT];
-    float vs = 0.f, vinv = 0.f;   // a power of two not below any s of V so far, and kOne / vs
-    bool flushed = false;
+      // the rows as B operand, a lane 2 G channels.  (Columns of rows that are not there hold what they held.)
+      for (int r = 0; r < n_rows; ++r) {
+        float v[2 * G], top = 0.f;
+        const long long from = (long long)(q.q0 + step_row(r)) * a.q_token + q_head(r) * a.q_head;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+        for (int i = 0; i < 2 * G; ++i) {
+          const int c = i * 32 + lane;
+          v[i] = c < s.head_dim ? load_as_float(a.q, a.dtype, from + c) : 0.f;
+          top = fmaxf(top, fabsf(v[i]));
+        }
 #pragma unroll
-      for (int g = 0; g < G; ++g)
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        int k = 0;
+        if (top > 0.f && top <= 3.402823466e38f) {
+          int e;
+          frexpf(top, &e);
+          k = (T == 2 ? 11 : 14) - e;
+        }
+        float part[G], first[G];   // sums of q 2^k and of its first term
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int g = 0; g < G; ++g) part[g] = first[g] = 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) O[n][g][i][e] = 0.f;
+        for (int i = 0; i < 2 * G; ++i) {
+          const int c = (i & 1) * 32 + lane, g = i >> 1, nib = c & 7;   // channel of the block, of its word
+          const float x = scalbnf(v[i], k);
+          const float odd = (nib & 1) ? 0.0625f : 1.f, hi = T == 2 ? rintf(x) : x, lo = T == 2 ? rintf((x - hi) * kLow) : 0.f;
+          part[g] += T == 2 ? lo : x;
+          first[g] += hi;
+          // word (c % 16) / 8 of lane c / 16: its two steps' registers (nib / 2) % 2, b0 or b1 nib % 2, half nib / 4
+          const int col = T == 2 ? (r & 3) * 2 : r & 7, nt = T == 2 ? r >> 2 : r >> 3;
+          __half* to = reinterpret_cast<__half*>(s_q + ((nt * G + g) * 2 + (c % 16) / 8) * 512 + (col * 4 + c / 16) * 16) + (nib / 2 % 2) * 4 +
+                       (nib & 1) * 2 + nib / 4;
+          *to = __float2half_rn(hi * odd);
+          if constexpr (T == 2) to[32] = __float2half_rn(lo * odd);   // the next column: 4 lanes of 16 bytes on
+        }
 #pragma unroll
-      for (int r = 0; r < kLR; ++r) {
-        m[n][r] = -INFINITY;
-        l[n][r] = 0.f;
-#pragma unroll
-        for (int g = 0; g < G; ++g) z[n][r][g] = 0.f;
-      }
-      m_flush[n] = -INFINITY;
-    }
-    auto row_of = [&](int n, int r) { return T == 2 ? n * 4 + t4 : n * 8 + t4 * 2 + r; };
-    int vis[NT][kLR];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int r = 0; r < kLR; ++r) vis[n][r] = sees(row_of(n, r));
-    const int least = sees(0), most = sees(n_rows - 1);
-
-    auto tile_pass = [&](uint32_t at, int tile, bool wrong, auto masked) {
-      constexpr bool kMasked = decltype(masked)::value;
-      const int pos = tile * kTile + gr;
-      float S[NT][kLR][2];
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int r = 0; r < kLR; ++r) S[n][r][0] = S[n][r][1] = 0.f;
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        const uint4 w = lds128(at + g * kBlockBytes + lane * 16);
-        const uint2 pw = lds64(at + g * kBlockBytes + kCodeBytes + gr * 8);
-        float acc[NT][4];
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t x = h ? w.y : w.x, y = h ? w.w : w.z;
-          const uint32_t x8 = x >> 8, y8 = y >> 8;
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const uint4 bq = lds128(s32(s_q) + ((n * G + g) * 2 + h) * 512 + lane * 16);
-            mma_f16(acc[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, bq.x, bq.y);
-            mma_f16(acc[n], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, bq.z, bq.w);
+        for (int g = 0; g < G; ++g) {
+          part[g] = warp_sum(part[g]);
+          if constexpr (T == 2) first[g] = warp_sum(first[g]);
+          if (lane == 0) {   // (all in units of the scores' sums: codes enter as code 2^-24)
+            s_sum[g * C::kRows + r] = (T == 2 ? fmaf(part[g], 1.f / kLow, first[g]) : part[g]) * 0x1p-24f;
+            s_start[(g * C::kRows + r) * 2] = (T == 2 ? first[g] : part[g]) * (-8.f * 0x1p-24f);
+            s_start[(g * C::kRows + r) * 2 + 1] = part[g] * (-8.f * 0x1p-24f);
           }
         }
-        const float2 p0 = unpack_half2(pw.x), p1 = unpack_half2(pw.y);   // (s, mid) of tokens gr and gr + 8
-        const float c0 = fmaf(-8.f, p0.x, p0.y), c1 = fmaf(-8.f, p1.x, p1.y);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int r = 0; r < kLR; ++r) {
-            const float qs = s_sum[g * kMaxRows + row_of(n, r)];
-            const float a0 = T == 2 ? acc[n][0] + acc[n][1] : acc[n][r], a1 = T == 2 ? acc[n][2] + acc[n][3] : acc[n][2 + r];
-            S[n][r][0] = fmaf(p0.x, a0, fmaf(c0, qs, S[n][r][0]));
-            S[n][r][1] = fmaf(p1.x, a1, fmaf(c1, qs, S[n][r][1]));
-          }
+        if (lane == 0) s_factor[r] = (float)fmin(ldexp((double)a.scale * 1.4426950408889634, 24 - k), 0x1p100);
       }
-      // pairs of V, their largest step, and whether a maximum has to move
-      const uint32_t v_at = at + G * kBlockBytes;
-      uint2 pv[G];
-      __half2 top0 = __half2half2(__ushort_as_half(0)), top1 = top0;
+      __syncwarp();
+
+      float O[NT][G][4][4], z[NT][kLR][G], m[NT][kLR], l[NT][kLR], m_flush[NT], factor[NT][kLR];
+      float vs = 0.f, vinv = 0.f;   // a power of two not below any s of V so far, and kOne / vs
+      bool flushed = false;
+      auto row_of = [&](int n, int r) { return T == 2 ? n * 4 + t4 : n * 8 + t4 * 2 + r; };
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        pv[g] = lds64(v_at + g * kBlockBytes + kCodeBytes + gr * 8);
-        if constexpr (kMasked) {   // (behind the last token lies anything)
-          if (pos >= q.len) pv[g].x = 0u;
-          if (pos + 8 >= q.len) pv[g].y = 0u;
-        }
-        if (wrong) pv[g] = make_uint2(0u, 0u);
-        top0 = __hmax2(top0, *reinterpret_cast<const __half2*>(&pv[g].x));
-        top1 = __hmax2(top1, *reinterpret_cast<const __half2*>(&pv[g].y));
-      }
-      const float step = fmaxf(__low2float(top0), __low2float(top1));
-      bool move = step > vs;
+      for (int n = 0; n < NT; ++n) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) O[n][g][i][e] = 0.f;
 #pragma unroll
         for (int r = 0; r < kLR; ++r) {
-          const float f = s_factor[row_of(n, r)];
+          m[n][r] = kNone;
+          l[n][r] = 0.f;
+          factor[n][r] = s_factor[row_of(n, r)];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            S[n][r][e] *= f;
-            if (wrong) S[n][r][e] = NAN;
-            if (kMasked && pos + 8 * e >= vis[n][r]) S[n][r][e] = -INFINITY;
-            move = move || S[n][r][e] > m[n][r] + kLazy;
-          }
+          for (int g = 0; g < G; ++g) z[n][r][g] = 0.f;
         }
-      if (__any_sync(0xffffffffu, move)) {
-        float largest = step;
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
-        const float next_vs = fmaxf(vs, __uint_as_float((__float_as_uint(largest) + 0x7FFFFFu) & 0x7F800000u));
-        const float v_keep = next_vs > 0.f ? vs / next_vs : 1.f;
-        vs = next_vs;
-        vinv = vs > 0.f ? kOne / vs : 0.f;
-        float keep[NT][kLR];
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int r = 0; r < kLR; ++r) {
-            float x = fmaxf(S[n][r][0], S[n][r][1]);
-#pragma unroll
-            for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-            const float next = fmaxf(m[n][r], x);
-            keep[n][r] = next == m[n][r] ? 1.f : exp2_fast(m[n][r] - next);
-            m[n][r] = next;
-            l[n][r] *= keep[n][r];
-#pragma unroll
-            for (int g = 0; g < G; ++g) z[n][r][g] *= keep[n][r];
-            keep[n][r] *= v_keep;
-          }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int g = 0; g < G; ++g)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) O[n][g][i][e] *= keep[n][kLR == 2 ? e & 1 : 0];
+        m_flush[n] = kNone;
       }
-      float p[NT][kLR][2];
+      const int least = sees(0), most = sees(n_rows - 1);
+
+      // N tiles; masked: one that some row does not see all of, or without a page
+      auto pass = [&](auto tiles, auto is_masked, const unsigned char* at0, const unsigned char* at1, int pos, bool wrong) {
+        constexpr int N = decltype(tiles)::value;
+        constexpr bool kMasked = decltype(is_masked)::value;
+        float S[N][NT][kLR][2];
+        uint2 pv[N][G];
+        __half2 steps = __half2half2(__ushort_as_half(0));
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+        for (int i = 0; i < N; ++i) {
+          const unsigned char* at = i ? at1 : at0;
 #pragma unroll
-        for (int r = 0; r < kLR; ++r) {
-          const float from = m[n][r] == -INFINITY ? 0.f : m[n][r];
+          for (int g = 0; g < G; ++g) {
+            const uint4 w = reinterpret_cast<const uint4*>(at + g * kBlockBytes)[lane];
+            const uint2 pw = reinterpret_cast<const uint2*>(at + g * kBlockBytes + kCodeBytes)[gr];
+            float acc[NT][4];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            p[n][r][e] = exp2_fast(S[n][r][e] - from);
-            l[n][r] += p[n][r][e];
-          }
-        }
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        const uint4 w = lds128(v_at + g * kBlockBytes + lane * 16);
-        const float2 p0 = unpack_half2(pv[g].x), p1 = unpack_half2(pv[g].y);
-        const float s0 = p0.x * vinv, s1 = p1.x * vinv;
-        uint32_t b0[NT], b1[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float x[kLR][2];
-#pragma unroll
-          for (int r = 0; r < kLR; ++r) {
-            x[r][0] = p[n][r][0] * s0;
-            x[r][1] = p[n][r][1] * s1;
-            float z0 = p[n][r][0] * p0.y, z1 = p[n][r][1] * p1.y;
-            if constexpr (kMasked) {   // (a token that this row does not see need not be a number)
-              if (pos >= vis[n][r]) x[r][0] = z0 = 0.f;
-              if (pos + 8 >= vis[n][r]) x[r][1] = z1 = 0.f;
+            for (int n = 0; n < NT; ++n) {
+              // -8 times the sum of the column's q: the sums are those of code - 8
+              if constexpr (T == 2) {
+                const float2 v = reinterpret_cast<const float2*>(s_start)[g * C::kRows + n * 4 + t4];
+                acc[n][0] = acc[n][2] = v.x;
+                acc[n][1] = acc[n][3] = v.y;
+              } else {
+                const float4 v = reinterpret_cast<const float4*>(s_start)[(g * C::kRows + n * 8) / 2 + t4];
+                acc[n][0] = acc[n][2] = v.x;
+                acc[n][1] = acc[n][3] = v.z;
+              }
             }
-            z[n][r][g] += z0 + z1;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t x = h ? w.y : w.x, y = h ? w.w : w.z;
+              const uint32_t x8 = x >> 8, y8 = y >> 8;
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                const uint4 bq = reinterpret_cast<const uint4*>(s_q + ((n * G + g) * 2 + h) * 512)[lane];
+                mma_f16(acc[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, bq.x, bq.y);
+                mma_f16(acc[n], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, bq.z, bq.w);
+              }
+            }
+            const float2 p0 = unpack_half2(pw.x), p1 = unpack_half2(pw.y);   // (s, mid) of tokens gr and gr + 8
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int r = 0; r < kLR; ++r) {
+                const float qs = s_sum[g * C::kRows + row_of(n, r)];
+                const float a0 = T == 2 ? fmaf(acc[n][1], 1.f / kLow, acc[n][0]) : acc[n][r];
+                const float a1 = T == 2 ? fmaf(acc[n][3], 1.f / kLow, acc[n][2]) : acc[n][2 + r];
+                S[i][n][r][0] = fmaf(p0.x, a0, g ? fmaf(p0.y, qs, S[i][n][r][0]) : p0.y * qs);
+                S[i][n][r][1] = fmaf(p1.x, a1, g ? fmaf(p1.y, qs, S[i][n][r][1]) : p1.y * qs);
+              }
+            // pairs of V, and their largest step
+            pv[i][g] = reinterpret_cast<const uint2*>(at + (G + g) * kBlockBytes + kCodeBytes)[gr];
+            if constexpr (kMasked) {   // (behind the last token lies anything)
+              if (wrong || pos + gr >= q.len) pv[i][g].x = 0u;
+              if (wrong || pos + gr + 8 >= q.len) pv[i][g].y = 0u;
+            }
+            steps = __hmax2(steps, __hmax2(*reinterpret_cast<const __half2*>(&pv[i][g].x), *reinterpret_cast<const __half2*>(&pv[i][g].y)));
           }
-          if constexpr (T == 2) {
-            const __half h0 = __float2half_rn(x[0][0]), h1 = __float2half_rn(x[0][1]);
-            b0[n] = pack_half2(__half2float(h0), x[0][0] - __half2float(h0));
-            b1[n] = pack_half2(__half2float(h1), x[0][1] - __half2float(h1));
-          } else {
-            b0[n] = pack_half2(x[0][0], x[kLR - 1][0]);
-            b1[n] = pack_half2(x[0][1], x[kLR - 1][1]);
-          }
-          b0[n] = transpose8x8(b0[n]);
-          b1[n] = transpose8x8(b1[n]);
         }
-        const uint32_t x8 = w.x >> 8, y8 = w.y >> 8, z8 = w.z >> 8, w8 = w.w >> 8;
-        const uint32_t A[4][4] = {{centred<false>(w.x), centred<false>(w.y), centred<false>(w.z), centred<false>(w.w)},
-                                  {centred<true>(w.x), centred<true>(w.y), centred<true>(w.z), centred<true>(w.w)},
-                                  {centred<false>(x8), centred<false>(y8), centred<false>(z8), centred<false>(w8)},
-                                  {centred<true>(x8), centred<true>(y8), centred<true>(z8), centred<true>(w8)}};
+        const float step = __low2float(steps);
+        bool move = step > vs;
+        float p[N][NT][kLR][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < N; ++i)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma_f16(O[n][g][i], A[i][0], A[i][1], A[i][2], A[i][3], b0[n], b1[n]);
-      }
-    };
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int r = 0; r < kLR; ++r) {
+              if constexpr (kMasked) {
+                const int vis = sees(row_of(n, r)) - pos - gr;
+                S[i][n][r][0] = vis <= 0 ? -INFINITY : wrong ? NAN : S[i][n][r][0];
+                S[i][n][r][1] = vis <= 8 ? -INFINITY : wrong ? NAN : S[i][n][r][1];
+              }
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                p[i][n][r][e] = fmaf(S[i][n][r][e], factor[n][r], -m[n][r]);
+                move = move || p[i][n][r][e] > kLazy;
+              }
+            }
+        if (__any_sync(0xffffffffu, move)) {
+          float largest = step;
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
+          const float next_vs = fmaxf(vs, __uint_as_float((__float_as_uint(largest) + 0x7FFFFFu) & 0x7F800000u));
+          const float v_keep = next_vs > 0.f ? vs / next_vs : 1.f;
+          vs = next_vs;
+          vinv = vs > 0.f ? kOne / vs : 0.f;
+          float keep[NT][kLR];
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int r = 0; r < kLR; ++r) {
+              float x = m[n][r];
+#pragma unroll
+              for (int i = 0; i < N; ++i) x = fmaxf(x, fmaxf(S[i][n][r][0] * factor[n][r], S[i][n][r][1] * factor[n][r]));
+#pragma unroll
+              for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+              if (x - m[n][r] <= kLazy) x = m[n][r];   // (another row's: this one's sums stay as they are)
+              keep[n][r] = exp2_fast(m[n][r] - x);
+              m[n][r] = x;
+              l[n][r] *= keep[n][r];
+#pragma unroll
+              for (int g = 0; g < G; ++g) z[n][r][g] *= keep[n][r];
+              keep[n][r] *= v_keep;
+#pragma unroll
+              for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) p[i][n][r][e] = fmaf(S[i][n][r][e], factor[n][r], -x);
+            }
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[n][g][i][e] *= keep[n][kLR == 2 ? e & 1 : 0];
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const unsigned char* at = (i ? at1 : at0) + G * kBlockBytes;
+          float ps[NT][kLR][2];
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int r = 0; r < kLR; ++r)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                p[i][n][r][e] = exp2_fast(p[i][n][r][e]);
+                l[n][r] += p[i][n][r][e];
+                ps[n][r][e] = p[i][n][r][e] * vinv;
+              }
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const uint4 w = reinterpret_cast<const uint4*>(at + g * kBlockBytes)[lane];
+            const float2 p0 = unpack_half2(pv[i][g].x), p1 = unpack_half2(pv[i][g].y);
+            uint32_t b0[NT], b1[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              float x[kLR][2];
+#pragma unroll
+              for (int r = 0; r < kLR; ++r) {
+                x[r][0] = ps[n][r][0] * p0.x;
+                x[r][1] = ps[n][r][1] * p1.x;
+                if constexpr (kMasked) {   // (a token that this row does not see need not be a number)
+                  const int vis = sees(row_of(n, r)) - pos - gr;
+                  if (vis <= 0) x[r][0] = 0.f;
+                  else z[n][r][g] = fmaf(p[i][n][r][0], p0.y, z[n][r][g]);
+                  if (vis <= 8) x[r][1] = 0.f;
+                  else z[n][r][g] = fmaf(p[i][n][r][1], p1.y, z[n][r][g]);
+                } else {
+                  z[n][r][g] = fmaf(p[i][n][r][1], p1.y, fmaf(p[i][n][r][0], p0.y, z[n][r][g]));
+                }
+              }
+              if constexpr (T == 2) {   // its upper eleven bits and the rest
+                const float h0 = __uint_as_float(__float_as_uint(x[0][0]) & 0xFFFFE000u), h1 = __uint_as_float(__float_as_uint(x[0][1]) & 0xFFFFE000u);
+                b0[n] = pack_half2(h0, x[0][0] - h0);
+                b1[n] = pack_half2(h1, x[0][1] - h1);
+              } else {
+                b0[n] = pack_half2(x[0][0], x[kLR - 1][0]);
+                b1[n] = pack_half2(x[0][1], x[kLR - 1][1]);
+              }
+              b0[n] = transpose8x8(b0[n]);
+              b1[n] = transpose8x8(b1[n]);
+            }
+            const uint32_t x8 = w.x >> 8, y8 = w.y >> 8, z8 = w.z >> 8, w8 = w.w >> 8;
+            const uint32_t A[4][4] = {{centred<false>(w.x), centred<false>(w.y), centred<false>(w.z), centred<false>(w.w)},
+                                      {centred<true>(w.x), centred<true>(w.y), centred<true>(w.z), centred<true>(w.w)},
+                                      {centred<false>(x8), centred<false>(y8), centred<false>(z8), centred<false>(w8)},
+                                      {centred<true>(x8), centred<true>(y8), centred<true>(z8), centred<true>(w8)}};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int n = 0; n < NT; ++n) mma_f16(O[n][g][k], A[k][0], A[k][1], A[k][2], A[k][3], b0[n], b1[n]);
+          }
+        }
+      };
 
-    // rows of the area: this warp's, row `r` (of kAreaRows), from channel 8 gr of block g on
-    auto area = [&](int w, int r, int g) { return s_area + (w * C::kAreaRows + r) * C::kAreaStride + g * kGroup + gr * 8; };
-    // channels 8 gr .. + 7 of block g: the four steps' rows gr, then their rows gr + 8
-    auto lane_sums = [&](int n, int g, int r, float (&v)[8]) {
-      const float f = vs * (1.f / kOne);
+      // the warp's part of a segment that it shares (or that it has to sum in pieces): channels 8 gr .. + 7 of a block
+      const bool tail = tile == 0;
+      float* part = a.parts + (2ll * share + tail) * C::kPart;
+      auto lane_sums = [&](int n, int g, int r, float (&v)[8]) {
+        const float f = vs * (1.f / kOne);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = (T == 2 ? O[n][g][i][0] + O[n][g][i][1] : O[n][g][i][r]) * f;
-        v[i + 4] = (T == 2 ? O[n][g][i][2] + O[n][g][i][3] : O[n][g][i][2 + r]) * f;
-      }
-    };
-    auto add_flushed = [&](int n, int g, float keep, float (&v)[8]) {   // (T = 2)
-      const float4* from = reinterpret_cast<const float4*>(area(warp, n * 4 + t4, g));
-      const float4 x = from[0], y = from[1];
-      v[0] = fmaf(x.x, keep, v[0]), v[1] = fmaf(x.y, keep, v[1]), v[2] = fmaf(x.z, keep, v[2]), v[3] = fmaf(x.w, keep, v[3]);
-      v[4] = fmaf(y.x, keep, v[4]), v[5] = fmaf(y.y, keep, v[5]), v[6] = fmaf(y.z, keep, v[6]), v[7] = fmaf(y.w, keep, v[7]);
-    };
-    auto to_area = [&](int r, int g, const float (&v)[8]) {
-      float4* to = reinterpret_cast<float4*>(area(warp, r, g));
-      to[0] = make_float4(v[0], v[1], v[2], v[3]);
-      to[1] = make_float4(v[4], v[5], v[6], v[7]);
-    };
+        for (int i = 0; i < 4; ++i) {
+          v[i] = (T == 2 ? O[n][g][i][0] + O[n][g][i][1] : O[n][g][i][r]) * f;
+          v[i + 4] = (T == 2 ? O[n][g][i][2] + O[n][g][i][3] : O[n][g][i][2 + r]) * f;
+        }
+        if (T == 2 && flushed) {
+          const float keep = exp2_fast(m_flush[n] - m[n][r]);
+          const float4* from = reinterpret_cast<const float4*>(part + row_of(n, r) * C::kDim + g * kGroup + gr * 8);
+          const float4 x = __ldcg(from), y = __ldcg(from + 1);
+          v[0] = fmaf(x.x, keep, v[0]), v[1] = fmaf(x.y, keep, v[1]), v[2] = fmaf(x.z, keep, v[2]), v[3] = fmaf(x.w, keep, v[3]);
+          v[4] = fmaf(y.x, keep, v[4]), v[5] = fmaf(y.y, keep, v[5]), v[6] = fmaf(y.z, keep, v[6]), v[7] = fmaf(y.w, keep, v[7]);
+        }
+      };
+      auto to_part = [&](int n, int g, int r, const float (&v)[8]) {
+        float4* to = reinterpret_cast<float4*>(part + row_of(n, r) * C::kDim + g * kGroup + gr * 8);
+        __stcg(to, make_float4(v[0], v[1], v[2], v[3]));
+        __stcg(to + 1, make_float4(v[4], v[5], v[6], v[7]));
+      };
 
-    int since = 0;
-    for (; j < mine; ++j) {
-      const long long at_u = u0 + warp + (long long)kWarps * j;
-      if (at_u >= upto) break;
-      const int stage = j % C::kStages;
-      if (!gave_up && !mbar_wait(bars + stage, (uint32_t)(j / C::kStages) & 1u)) gave_up = true;
-      gave_up = __any_sync(0xffffffffu, gave_up);
-      const int tile = (int)(at_u - begin);
-      if (tile * kTile < most && !gave_up) {
-        const bool wrong = bad[(j >> 5) & 1] >> (j & 31) & 1u;
-        if (wrong && lane == 0) ctl->status = GSI_ERR_INVALID_ARG;
-        const uint32_t at = ring + stage * C::kTileBytes;
-        if ((tile + 1) * kTile <= least) tile_pass(at, tile, wrong, std::false_type{});
-        else tile_pass(at, tile, wrong, std::true_type{});
-        if (T == 2 && ++since == kFlush) {
+      const int end = j + n_tiles;
+      int since = 0;
+      for (int pos = tile * kTile; j < end;) {
+        const unsigned char* at0 = arrived();
+        if (C::kPair == 2 && j + 1 < end && least - pos >= 2 * kTile) {   // (the tiles of a page that is not there are in neither)
+          const unsigned missing = ((j & 32) ? bad_odd : bad_even) >> (j & 31) & 1u, missing1 = ((j + 1 & 32) ? bad_odd : bad_even) >> (j + 1 & 31) & 1u;
+          if (!(missing | missing1)) {
+            const unsigned char* at1 = arrived();
+            if (gave_up) break;
+            pass(std::integral_constant<int, C::kPair>{}, std::false_type{}, at0, at1, pos, false);
+            __syncwarp();
+            issue();
+            issue();
+            j += 2;
+            pos += 2 * kTile;
+            since += 2;
+            goto summed;
+          }
+        }
+        if (gave_up) break;
+        if (pos < most) {
+          const bool wrong = ((j & 32) ? bad_odd : bad_even) >> (j & 31) & 1u;
+          if (wrong && lane == 0) ctl->status = GSI_ERR_INVALID_ARG;
+          if (C::kPair == 1 && least - pos >= kTile && !wrong) pass(std::integral_constant<int, 1>{}, std::false_type{}, at0, at0, pos, false);
+          else pass(std::integral_constant<int, 1>{}, std::true_type{}, at0, at0, pos, wrong);
+          ++since;
+        }
+        __syncwarp();
+        issue();
+        ++j;
+        pos += kTile;
+      summed:
+        if (T == 2 && since >= kFlush && j < end) {
           since = 0;
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            const float keep = m_flush[n] == -INFINITY ? 0.f : exp2_fast(m_flush[n] - m[n][0]);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
               float v[8];
               lane_sums(n, g, 0, v);
-              if (flushed) add_flushed(n, g, keep, v);
-              to_area(n * 4 + t4, g, v);
+              to_part(n, g, 0, v);
 #pragma unroll
               for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -545,148 +605,155 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
           flushed = true;
         }
       }
-      __syncwarp();
-      if (!gave_up) issue();
-    }
+      if (gave_up) {
+        if (lane == 0) ctl->status = GSI_ERR_TIMEOUT;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < kLR; ++r) l[n][r] = NAN;
+      }
 
-    // ---- the warps' sums, and those of the CTAs that share the segment
-    if (gave_up) {
-      if (lane == 0) ctl->status = GSI_ERR_TIMEOUT;
+      // ---- the segment's sums: out, where they are the whole of it
+      const bool whole = tail && n_tiles == q.tiles;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int r = 0; r < kLR; ++r) l[n][r] = NAN;
-    }
+        for (int r = 0; r < kLR; ++r) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+          for (int o = 4; o < 32; o <<= 1) {
+            l[n][r] += __shfl_xor_sync(0xffffffffu, l[n][r], o);
 #pragma unroll
-      for (int r = 0; r < kLR; ++r) {
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
-          l[n][r] += __shfl_xor_sync(0xffffffffu, l[n][r], o);
-#pragma unroll
-          for (int g = 0; g < G; ++g) z[n][r][g] += __shfl_xor_sync(0xffffffffu, z[n][r][g], o);
-        }
-        if (gr == 0) {
-          s_m[warp * kMaxRows + row_of(n, r)] = m[n][r];
-          s_l[warp * kMaxRows + row_of(n, r)] = l[n][r];
-        }
-      }
-    const bool whole = u == begin && upto == end;
-    float* part = a.parts + ((long long)b * 2 + (begin >= u0)) * C::kPart;
-    constexpr int kPasses = T == 2 ? 1 : NT * 2;
-#pragma unroll
-    for (int pass = 0; pass < kPasses; ++pass) {
-      // area row i of the pass is row `base_row + i * stride` of the tile
-      const int base_row = T == 2 ? 0 : pass / 2 * 8 + (pass & 1);
-      constexpr int kStride = T == 2 ? 1 : 2;
-      if (base_row >= n_rows) break;
-      if constexpr (T == 2) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const float keep = m_flush[n] == -INFINITY ? 0.f : exp2_fast(m_flush[n] - m[n][0]);
+            for (int g = 0; g < G; ++g) z[n][r][g] += __shfl_xor_sync(0xffffffffu, z[n][r][g], o);
+          }
+          const int row = row_of(n, r);
+          if (row >= n_rows) continue;
+          const long long to = (long long)(q.q0 + step_row(row)) * a.out_token + q_head(row) * a.out_head;
+          const float over = l[n][r] == 0.f ? 0.f : 1.f / l[n][r];   // (no token seen: 0)
 #pragma unroll
           for (int g = 0; g < G; ++g) {
             float v[8];
-            lane_sums(n, g, 0, v);
-            if (flushed) add_flushed(n, g, keep, v);
+            lane_sums(n, g, r, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += z[n][0][g];
-            if (n * 4 + t4 < n_rows) to_area(n * 4 + t4, g, v);
+            for (int i = 0; i < 8; ++i) v[i] += z[n][r][g];
+            if (whole) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int c = g * kGroup + gr * 8 + i;
+                if (c < s.head_dim) store_from_float(a.out, a.dtype, to + c, v[i] * over);
+              }
+            } else {
+              to_part(n, g, r, v);
+            }
           }
+          if (!whole && gr == 0) __stcg(reinterpret_cast<float2*>(part + C::kRows * C::kDim) + row, make_float2(m[n][r], l[n][r]));
         }
-      } else {
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          float v[8];
-          lane_sums(pass / 2, g, pass & 1, v);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] += z[pass / 2][pass & 1][g];
-          to_area(t4, g, v);
-        }
-      }
-      __syncthreads();
-      const int rows = min(C::kAreaRows, (n_rows - base_row + kStride - 1) / kStride);
-      for (int i = tid; i < rows * C::kDim; i += kThreads) {
-        const int ar = i / C::kDim, c = i - ar * C::kDim, r = base_row + ar * kStride;
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w * kMaxRows + r]);
-        const float from = top == -INFINITY ? 0.f : top;
-        float sum_l = 0.f, v = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float mw = s_m[w * kMaxRows + r], lw = s_l[w * kMaxRows + r];
-          if (mw == -INFINITY && lw == 0.f) continue;   // (it saw nothing)
-          const float f = exp2_fast(mw - from);
-          sum_l += lw * f;
-          v += s_area[(w * C::kAreaRows + ar) * C::kAreaStride + c] * f;
-        }
-        if (whole) {
-          if (c < s.head_dim)
-            store_from_float(a.out, a.dtype, (q.q0 + step_row(r)) * a.out_token + q_head(r) * a.out_head + c, sum_l == 0.f ? 0.f : v / sum_l);
-        } else {
-          __stcg(part + r * C::kDim + c, v);
-          if (c == 0) {
-            __stcg(part + kMaxRows * C::kDim + r, top);
-            __stcg(part + kMaxRows * (C::kDim + 1) + r, sum_l);
-          }
-        }
-      }
-      __syncthreads();
-    }
-    if (!whole) {
-      // the boundaries between shares that lie within the segment: shares first_b .. first_b + n_parts - 1 have a part
-      const long long b1 = ((begin + kSnap) * shares + total.a - 1) / total.a, b2 = ((end - kSnap + 1) * shares + total.a - 1) / total.a - 1;
-      const int first_b = (int)b1 - 1, n_parts = (int)(b2 - b1) + 2;
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) {
-        s_last = atomicAdd(a.tickets + first_b, 1u) == (unsigned)n_parts - 1;
-        if (s_last) a.tickets[first_b] = 0u;
-      }
-      __syncthreads();
-      if (s_last) {
+      if (!whole) {
+        // the boundaries between shares that lie within the segment: shares first .. first + n_parts - 1 have a part
+        const long long begin = u0 + (end - n_tiles) - tile, behind = begin + q.tiles;   // (end: of the piece, in tiles of the share)
+        const long long b1 = ((begin + kSnap) * shares + total.a - 1) / total.a, b2 = ((behind - kSnap + 1) * shares + total.a - 1) / total.a - 1;
+        const int first = (int)b1 - 1, n_parts = (int)(b2 - b1) + 2;
         __threadfence();
-        for (int i = tid; i < n_rows * C::kDim; i += kThreads) {
-          const int r = i / C::kDim, c = i - r * C::kDim;
-          float top = -INFINITY, sum_l = 0.f, v = 0.f;
-          for (int x0 = 0; x0 < n_parts; x0 += 8) {
-            float pm[8], pl[8], px[8];
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              const float* from = a.parts + ((long long)(first_b + min(x0 + x, n_parts - 1)) * 2 + (x0 + x == 0)) * C::kPart;
-              pm[x] = __ldcg(from + kMaxRows * C::kDim + r);
-              pl[x] = __ldcg(from + kMaxRows * (C::kDim + 1) + r);
-              px[x] = __ldcg(from + r * C::kDim + c);
-            }
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              if (x0 + x >= n_parts || (pm[x] == -INFINITY && pl[x] == 0.f)) continue;
-              const float next = fmaxf(top, pm[x]), from = next == -INFINITY ? 0.f : next;
-              const float keep = exp2_fast(top - from), f = exp2_fast(pm[x] - from);
-              top = next;
-              sum_l = sum_l * keep + pl[x] * f;
-              v = v * keep + px[x] * f;
-            }
+        __syncwarp();
+        bool last = false;
+        if (lane == 0) {
+          last = atomicAdd(a.tickets + first, 1u) == (unsigned)n_parts - 1;
+          if (last) {
+            a.tickets[first] = 0u;
+            __threadfence();
+            Pending& x = s_pending[atomicAdd(&s_n_pending, 1)];
+            x.first = first;
+            x.parts = n_parts;
+            x.rows = n_rows;
+            for (int r = 0; r < n_rows; ++r) x.out[r] = (long long)(q.q0 + step_row(r)) * a.out_token + q_head(r) * a.out_head;
           }
-          if (c < s.head_dim)
-            store_from_float(a.out, a.dtype, (q.q0 + step_row(r)) * a.out_token + q_head(r) * a.out_head + c, sum_l == 0.f ? 0.f : v / sum_l);
         }
+      }
+      // the next segment
+      tile += n_tiles;
+      if (tile == q.tiles) {
+        tile = 0;
+        if (++row_tile == q.n_row_tiles) {
+          row_tile = 0;
+          if (++head == s.n_heads) {
+            head = 0;
+            if (end < mine) do q = load_seq<C::kRows>(s, a, ++seq);
+              while (q.n_row_tiles == 0);
+          }
+        }
+      }
+    }
+    if (gave_up) {
+      // (copies in flight land before the block's memory is another's)
+      for (int i = 0; i < C::kStages; ++i) {
+        mbar_wait(bars + stage, phase);
+        if (++stage == C::kStages) {
+          stage = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+  }
+
+  // ---- segments that several warps share, by the block of the last of them: its threads take four channels each of
+  // every kSets-th part
+  __syncthreads();
+  constexpr int kLanes = C::kDim / 4, kSets = kThreads / kLanes / (kThreads % kLanes ? 2 : 1);
+  float4* s_v = reinterpret_cast<float4*>(smem);                      // [kSets][kLanes]
+  float2* s_ml = reinterpret_cast<float2*>(smem + kSets * kLanes * 16);   // [kSets]
+  const int n_pending = s_n_pending, set = tid / kLanes, c4 = tid - set * kLanes;
+  for (int i = 0; i < n_pending; ++i) {
+    const Pending& x = s_pending[i];
+    for (int r = 0; r < x.rows; ++r) {
+      if (set < kSets) {
+        float top = kNone, all = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int y0 = set; y0 < x.parts; y0 += 4 * kSets) {
+          float2 ml[4];
+          float4 px[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int b = min(y0 + y * kSets, x.parts - 1);
+            const float* from = a.parts + (2ll * (x.first + b) + (b == 0)) * C::kPart;
+            ml[y] = __ldcg(reinterpret_cast<const float2*>(from + C::kRows * C::kDim) + r);
+            px[y] = __ldcg(reinterpret_cast<const float4*>(from + r * C::kDim) + c4);
+          }
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            if (y0 + y * kSets >= x.parts) continue;
+            const float next = fmaxf(top, ml[y].x), keep = exp2_fast(top - next), f = exp2_fast(ml[y].x - next);
+            top = next;
+            all = all * keep + ml[y].y * f;
+            v.x = v.x * keep + px[y].x * f, v.y = v.y * keep + px[y].y * f;
+            v.z = v.z * keep + px[y].z * f, v.w = v.w * keep + px[y].w * f;
+          }
+        }
+        s_v[set * kLanes + c4] = v;
+        if (c4 == 0) s_ml[set] = make_float2(top, all);
+      }
+      __syncthreads();
+      if (set == 0) {
+        float top = kNone, all = 0.f;
+        for (int y = 0; y < kSets; ++y) top = fmaxf(top, s_ml[y].x);
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int y = 0; y < kSets; ++y) {
+          const float f = exp2_fast(s_ml[y].x - top);
+          const float4 w = s_v[y * kLanes + c4];
+          all += s_ml[y].y * f;
+          v[0] += w.x * f, v[1] += w.y * f, v[2] += w.z * f, v[3] += w.w * f;
+        }
+        for (int e = 0; e < 4; ++e)
+          if (c4 * 4 + e < s.head_dim) store_from_float(a.out, a.dtype, x.out[r] + c4 * 4 + e, all == 0.f ? 0.f : v[e] / all);
       }
       __syncthreads();
     }
-    u = upto;
   }
-  if (gave_up)   // (copies in flight land before the block's memory is another's)
-    for (int i = j; i < issued; ++i) mbar_wait(bars + i % C::kStages, (uint32_t)(i / C::kStages) & 1u);
 }
 
 template <int G, int T, int NT>
 cudaError_t launch(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
   using C = Cfg<G, T, NT>;
-  static_assert(C::kSmem <= 113 * 1024, "two blocks of an SM");
-  static_assert(C::kRows <= kMaxRows && C::kRing % 16 == 0 && C::kArea % 16 == 0 && (C::kSums + C::kMl) % 8 == 0, "layout");
+  static_assert(C::kSmem + 5120 <= 115712, "two blocks of an SM, with what else they hold in shared memory");
+  static_assert(C::kRows <= kMaxRows && C::kTileBytes % 16 == 0 && C::kSums % 16 == 0 && C::kPart <= kPartFloats(G), "layout");
   if (!a.q) return cudaFuncSetAttribute(k_kv_attend<G, T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   k_kv_attend<G, T, NT><<<kGrid, kThreads, C::kSmem, stream>>>(s, a, ctl);
   return cudaGetLastError();

@@ -111,7 +111,8 @@ def attend(q, k, v, scale, sixteen):
 
     Returns the output [D] and what a kernel may be off by, apart from the output's own rounding.  With u the half step
     of the operands (2^-23 for two f16 terms, 2^-12 for one):
-      scores: q in two terms is off by u (16-bit types are exact); the tensor cores truncate, at most one step of 2^-23 of
+      scores: an fp32 q is off by 2^-24 of its largest channel, and the sums of codes and q are exact; a 16-bit q is exact, and
+      the tensor cores truncate, at most one step of 2^-23 of
       the sum of the terms' sizes per instruction and fp32 addition, 4 and 2 for each 64 channels, 24 at most, and three
       roundings of the scaling; the sizes are those of q x (code s) and of the offset mid - 8 s;
       probabilities: e^x is off by 2^-22 and by the rounding of its argument, 3 x 2^-24 |score|; the rounding to the
@@ -129,7 +130,9 @@ def attend(q, k, v, scale, sixteen):
     q = q.astype(np.float64)
     score = kv[0] @ q * scale
     size = ks[0] @ np.abs(q) * abs(scale)
-    off = size * ((0 if sixteen else 2.0 ** -22) + 27 * 2.0 ** -23)
+    off = size * 27 * 2.0 ** -23
+    if not sixteen:
+        off = off + ks[0].sum(1) * np.abs(q).max() * abs(scale) * 2.0 ** -24
     p = np.exp(score - score.max())
     total = p.sum()
     p = p / total
