@@ -68,7 +68,7 @@ struct AttendArgs {
   gsi_dtype_t dtype;
   long long q_token, q_head, out_token, out_head;
   int n_rows, n_q_heads, shared;   // shared: q heads of a head of the cache
-  float scale;
+  float scale;   // of scores in powers of two
   const int *q_start, *kv_len, *table;
   int n_seqs;
   const unsigned char* pages;

@@ -51,9 +51,10 @@ struct Cfg {
   static constexpr int kRows = NT * 8 / T;           // rows of a warp
   static constexpr int kLaneRows = T == 1 ? 2 : 1;   // ... of a lane per column tile
   static constexpr int kTileBytes = G * 2 * kBlockBytes;
-  static constexpr int kStages = G == 1 ? 8 : G == 2 ? 4 : 2;
-  static constexpr int kPair = G * NT <= 2 ? 2 : 1;  // tiles in one pass, where registers have room
-  static constexpr int kRing = kStages * kTileBytes;
+  static constexpr int kPair = G * NT <= 2 ? 2 : 1;    // tiles in one pass, where registers have room
+  static constexpr int kBoth = G <= 2 ? 2 : 1;         // tiles of a stage
+  static constexpr int kStages = G == 1 ? 4 : 2;
+  static constexpr int kRing = kStages * kBoth * kTileBytes;
   static constexpr int kQ = NT * G * 1024;
   static constexpr int kSums = (3 * G + 1) * kRows * 4;   // per block: the sum of q and -8 times its terms'; factors of the scores
   static constexpr int kBars = kStages * 8;
@@ -85,7 +86,8 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 // Nibbles 0 and 4 (kOdd: 1 and 5) of a word, minus 8, as f16.
 template <bool kOdd>
 __device__ __forceinline__ uint32_t centred(uint32_t w) {
-  const uint32_t v = (w & (kOdd ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;   // 1024 + code (16 code)
+  uint32_t v;   // 1024 + code (16 code): (w & mask) | 1024
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(v) : "r"(w), "r"(kOdd ? 0x00F000F0u : 0x000F000Fu), "r"(0x64006400u));
   __half2 h = *reinterpret_cast<const __half2*>(&v);
   if constexpr (kOdd) h = __hfma2(h, __half2half2(__ushort_as_half(0x2C00)), __half2half2(__ushort_as_half(0xD480)));   // / 16 - 72
   else h = __hadd2(h, __half2half2(__ushort_as_half(0xE408)));   // - 1032
@@ -141,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_factor + C::kRows);
 
   if (lane == 0)
-    for (int i = 0; i < C::kStages; ++i) mbar_init(bars + i, 1);
+    for (int i = 0; i < C::kStages; ++i) mbar_init(bars + i, C::kBoth);
   for (int i = lane; i < (C::kQ + C::kSums) / 4; i += 32) reinterpret_cast<uint32_t*>(s_q)[i] = 0u;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   if (tid == 0) s_n_pending = 0;
@@ -240,19 +242,19 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       if (batch & 1) bad_odd = mask;
       else bad_even = mask;
     };
-    int issued = 0, to_stage = 0;
+    int issued = 0, to_stage = 0;   // tiles, a stage's at a time
     auto issue = [&]() {
       if (issued >= mine) return;
       if ((issued & 31) == 0) look_up(issued >> 5);
-      if (lane == (issued & 31)) {
+      if ((lane & -C::kBoth) == (issued & 31)) {
         if (where) {
           mbar_expect_tx(bars + to_stage, C::kTileBytes);
-          copy_tile(s32(ring) + to_stage * C::kTileBytes, where, C::kTileBytes, bars + to_stage);
+          copy_tile(s32(ring) + (to_stage * C::kBoth + (lane & (C::kBoth - 1))) * C::kTileBytes, where, C::kTileBytes, bars + to_stage);
         } else {
           mbar_arrive(bars + to_stage);
         }
       }
-      ++issued;
+      issued += C::kBoth;
       if (++to_stage == C::kStages) to_stage = 0;
     };
     for (int i = 0; i < C::kStages; ++i) issue();
@@ -260,14 +262,22 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
     int stage = 0;
     uint32_t phase = 0;
     bool gave_up = false;    // a copy did not arrive
-    auto arrived = [&]() {   // the next tile; its place
+    const unsigned char* at = ring;   // the stage that has arrived
+    // Tile j (the next): waits where it is the first of a stage.
+    auto arrive = [&](int j) {
+      if (j & (C::kBoth - 1)) return;
       if (__any_sync(0xffffffffu, !mbar_wait(bars + stage, phase))) gave_up = true;
-      const unsigned char* at = ring + stage * C::kTileBytes;
+      at = ring + stage * C::kBoth * C::kTileBytes;
+    };
+    // Tiles before j are read: the stage goes back where they were its last.
+    auto hand_back = [&](int j) {
+      if (j & (C::kBoth - 1)) return;
+      __syncwarp();
+      issue();
       if (++stage == C::kStages) {
         stage = 0;
         phase ^= 1u;
       }
-      return at;
     };
 
     // ---- segments of the share
@@ -291,19 +301,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        int k = 0;
-        if (top > 0.f && top <= 3.402823466e38f) {
-          int e;
-          frexpf(top, &e);
-          k = (T == 2 ? 11 : 14) - e;
-        }
+        // 2^k takes the largest to below 2^11 (2^14), as a product of two; a row of zeros, or with an infinity, stays as it is
+        int k = (T == 2 ? 137 : 140) - (int)(__float_as_uint(top) >> 23);
+        if (top == 0.f || top > 3.402823466e38f) k = 0;
+        const float k0 = __uint_as_float((uint32_t)(127 + k / 2) << 23), k1 = __uint_as_float((uint32_t)(127 + k - k / 2) << 23);
         float part[G], first[G];   // sums of q 2^k and of its first term
 #pragma unroll
         for (int g = 0; g < G; ++g) part[g] = first[g] = 0.f;
 #pragma unroll
         for (int i = 0; i < 2 * G; ++i) {
           const int c = (i & 1) * 32 + lane, g = i >> 1, nib = c & 7;   // channel of the block, of its word
-          const float x = scalbnf(v[i], k);
+          const float x = v[i] * k0 * k1;
           const float odd = (nib & 1) ? 0.0625f : 1.f, hi = T == 2 ? rintf(x) : x, lo = T == 2 ? rintf((x - hi) * kLow) : 0.f;
           part[g] += T == 2 ? lo : x;
           first[g] += hi;
@@ -324,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
             s_start[(g * C::kRows + r) * 2 + 1] = part[g] * (-8.f * 0x1p-24f);
           }
         }
-        if (lane == 0) s_factor[r] = (float)fmin(ldexp((double)a.scale * 1.4426950408889634, 24 - k), 0x1p100);
+        if (lane == 0) s_factor[r] = fminf(fmaxf(a.scale / k0 * (0x1p24f / k1), -0x1p100f), 0x1p100f);
       }
       __syncwarp();
 
@@ -353,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       const int least = sees(0), most = sees(n_rows - 1);
 
       // N tiles; masked: one that some row does not see all of, or without a page
-      auto pass = [&](auto tiles, auto is_masked, const unsigned char* at0, const unsigned char* at1, int pos, bool wrong) {
+      auto pass = [&](auto tiles, auto is_masked, const unsigned char* first, int pos, bool wrong) {
         constexpr int N = decltype(tiles)::value;
         constexpr bool kMasked = decltype(is_masked)::value;
         float S[N][NT][kLR][2];
@@ -361,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
         __half2 steps = __half2half2(__ushort_as_half(0));
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const unsigned char* at = i ? at1 : at0;
+          const unsigned char* at = first + i * C::kTileBytes;
 #pragma unroll
           for (int g = 0; g < G; ++g) {
             const uint4 w = reinterpret_cast<const uint4*>(at + g * kBlockBytes)[lane];
@@ -472,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const unsigned char* at = (i ? at1 : at0) + G * kBlockBytes;
+          const unsigned char* at = first + i * C::kTileBytes + G * kBlockBytes;
           float ps[NT][kLR][2];
 #pragma unroll
           for (int n = 0; n < NT; ++n)
@@ -557,35 +565,27 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       const int end = j + n_tiles;
       int since = 0;
       for (int pos = tile * kTile; j < end;) {
-        const unsigned char* at0 = arrived();
-        if (C::kPair == 2 && j + 1 < end && least - pos >= 2 * kTile) {   // (the tiles of a page that is not there are in neither)
-          const unsigned missing = ((j & 32) ? bad_odd : bad_even) >> (j & 31) & 1u, missing1 = ((j + 1 & 32) ? bad_odd : bad_even) >> (j + 1 & 31) & 1u;
-          if (!(missing | missing1)) {
-            const unsigned char* at1 = arrived();
-            if (gave_up) break;
-            pass(std::integral_constant<int, C::kPair>{}, std::false_type{}, at0, at1, pos, false);
-            __syncwarp();
-            issue();
-            issue();
-            j += 2;
-            pos += 2 * kTile;
-            since += 2;
-            goto summed;
-          }
-        }
+        arrive(j);
         if (gave_up) break;
-        if (pos < most) {
-          const bool wrong = ((j & 32) ? bad_odd : bad_even) >> (j & 31) & 1u;
-          if (wrong && lane == 0) ctl->status = GSI_ERR_INVALID_ARG;
-          if (C::kPair == 1 && least - pos >= kTile && !wrong) pass(std::integral_constant<int, 1>{}, std::false_type{}, at0, at0, pos, false);
-          else pass(std::integral_constant<int, 1>{}, std::true_type{}, at0, at0, pos, wrong);
-          ++since;
+        const unsigned missing = ((j & 32) ? bad_odd : bad_even) >> (j & 31);   // tiles from j on that have no page
+        if (C::kPair == 2 && !(j & 1) && j + 1 < end && least - pos >= 2 * kTile && !(missing & 3u)) {
+          pass(std::integral_constant<int, C::kPair>{}, std::false_type{}, at, pos, false);
+          j += 2;
+          pos += 2 * kTile;
+          since += 2;
+        } else {
+          if (pos < most) {
+            const bool wrong = missing & 1u;
+            if (wrong && lane == 0) ctl->status = GSI_ERR_INVALID_ARG;
+            const unsigned char* one = at + (j & (C::kBoth - 1)) * C::kTileBytes;
+            if (C::kPair == 1 && least - pos >= kTile && !wrong) pass(std::integral_constant<int, 1>{}, std::false_type{}, one, pos, false);
+            else pass(std::integral_constant<int, 1>{}, std::true_type{}, one, pos, wrong);
+            ++since;
+          }
+          ++j;
+          pos += kTile;
         }
-        __syncwarp();
-        issue();
-        ++j;
-        pos += kTile;
-      summed:
+        hand_back(j);
         if (T == 2 && since >= kFlush && j < end) {
           since = 0;
 #pragma unroll
