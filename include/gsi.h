@@ -479,7 +479,7 @@ typedef struct {
   int page_tokens; /* a multiple of 16, up to 4096                                  */
   int n_pages;     /* pages of a pool; n_pages * page_tokens < 2^31                 */
   int max_seqs;    /* 1..GSI_KV_MAX_SEQS                                            */
-  int max_pages;   /* pages of one sequence: the table's row; max_pages * page_tokens < 2^31 */
+  int max_pages;   /* pages of one sequence: the table's row; max_pages * page_tokens <= 2^30 */
   int max_tokens;  /* new tokens of a step: the length of slots and positions       */
 } gsi_kv_desc_t;
 

@@ -416,7 +416,7 @@ gsi_status_t make_shape(const gsi_kv_desc_t* d, kv::Shape* s) {
   if (d->n_heads <= 0 || d->head_dim <= 0 || d->page_tokens <= 0 || d->n_pages <= 0 || d->max_seqs <= 0 || d->max_pages <= 0 || d->max_tokens <= 0)
     return GSI_ERR_INVALID_ARG;
   if (d->head_dim > GSI_KV_MAX_DIM || d->n_heads > 65536 || d->page_tokens % kv::kTile || d->page_tokens > 4096 || d->max_seqs > GSI_KV_MAX_SEQS ||
-      (long long)d->n_pages * d->page_tokens >= 1ll << 31 || (long long)d->max_pages * d->page_tokens >= 1ll << 31)
+      (long long)d->n_pages * d->page_tokens >= 1ll << 31 || (long long)d->max_pages * d->page_tokens > 1ll << 30)
     return GSI_ERR_UNSUPPORTED;
   s->n_heads = d->n_heads;
   s->head_dim = d->head_dim;

@@ -37,30 +37,33 @@ using umma::s32;
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kGrid = kMaxShares / kWarps;   // two blocks an SM
-constexpr int kFlush = 32;      // tiles between sums in fp32 (T = 2)
-constexpr int kSnap = 4;        // tiles: the share of a warp ends with a segment that ends as near
+constexpr int kFlush = 32;      // units between sums in fp32 (T = 2)
 constexpr float kLow = 4096.f;  // units of the second term of q in one of the first
 constexpr float kLazy = 8.f;    // a running maximum is left where it is while 2^score stays below 2^kLazy above it
 constexpr float kOne = 64.f;    // p s <= 2^kLazy kOne s / vs < 2^15
 constexpr float kNone = -3e38f; // the maximum of no score
 
-// G: blocks of 64 channels; T: f16 terms of an operand; NT: column tiles of eight
-template <int G, int T, int NT>
+// G: blocks of 64 channels; T: f16 terms of an operand; NT: column tiles of eight; L: lane quarters of a tile.
+// A unit of work is 4 / L tiles of tokens of one head and a tile of rows: the columns of a column tile are 2 L for each
+// of them, so that lane quarter t has the scores of tile t / L (rows t % L, T = 2; 2 (t % L) and the next, T = 1).
+// Few rows so share the scalar work of a tile's scores, where they would leave most columns empty.
+template <int G, int T, int L, int NT>
 struct Cfg {
   static constexpr int kDim = G * kGroup;
-  static constexpr int kRows = NT * 8 / T;           // rows of a warp
-  static constexpr int kLaneRows = T == 1 ? 2 : 1;   // ... of a lane per column tile
-  static constexpr int kTileBytes = G * 2 * kBlockBytes;
-  static constexpr int kPair = G * NT <= 2 ? 2 : 1;    // tiles in one pass, where registers have room
-  static constexpr int kBoth = G <= 2 ? 2 : 1;         // tiles of a stage
-  static constexpr int kStages = G == 1 ? 4 : 2;
-  static constexpr int kRing = kStages * kBoth * kTileBytes;
+  static constexpr int kTiles = 4 / L;                 // of a unit
+  static constexpr int kLaneRows = T == 1 ? 2 : 1;     // rows of a lane per column tile
+  static constexpr int kRows = NT * L * kLaneRows;     // rows of a unit
+  static constexpr int kHalf = G * kBlockBytes;        // K of a tile, or V
+  static constexpr int kStages = (G == 1 ? 8 : G == 2 ? 4 : 2) / kTiles;   // units under way
+  static constexpr int kRing = kStages * kTiles * 2 * kHalf;
   static constexpr int kQ = NT * G * 1024;
-  static constexpr int kSums = (3 * G + 1) * kRows * 4;   // per block: the sum of q and -8 times its terms'; factors of the scores
-  static constexpr int kBars = kStages * 8;
+  static constexpr int kSums = ((3 * G + 1) * kRows * 4 + 15) / 16 * 16;   // per block: -8 times the sums of q's terms, the sum of q; factors
+  static constexpr int kBars = kStages * 2 * 8;
   static constexpr int kWarpBytes = (kRing + kQ + kSums + kBars + 15) / 16 * 16;
   static constexpr int kSmem = kWarps * kWarpBytes;
-  static constexpr int kPart = kRows * (kDim + 8);   // floats of a part: sums, then (maximum, sum of p) of the rows
+  static constexpr int kSnap = kTiles == 1 ? 4 : 2;    // units: the share of a warp ends with a segment that ends as near
+  static constexpr int kPart = kPartFloats(G);
+  static constexpr int kPartRows = kPart / (kDim + 8);
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -99,12 +102,19 @@ __device__ __forceinline__ void copy_tile(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-// What a step has of one sequence.  Units of work: (head, tile of rows, tile of tokens), the last the fastest.
+// What a step has of one sequence.  Its units: (head, tile of rows, tokens), the last the fastest; those of one head and
+// tile of rows are a segment.
 struct Seq {
-  int q0, m, len, seen, tiles, n_row_tiles;   // seen: by the row before its first
+  int q0, m, len, seen, units, n_row_tiles;   // seen: by the row before its first; units: of a segment
   __device__ __forceinline__ long long segments(const Shape& s) const { return (long long)n_row_tiles * s.n_heads; }
+  __device__ __forceinline__ long long all(const Shape& s) const { return segments(s) * units; }
 };
-template <int kRows>
+// a / b of numbers that are not negative and seldom large
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  if ((a | b) >> 32) return a / b;
+  return (unsigned)a / (unsigned)b;
+}
+template <int kRows, int kTiles>
 __device__ __forceinline__ Seq load_seq(const Shape& s, const AttendArgs& a, int i) {
   Seq q;
   q.q0 = __ldg(a.q_start + i);
@@ -114,7 +124,7 @@ __device__ __forceinline__ Seq load_seq(const Shape& s, const AttendArgs& a, int
   q.seen = q.m ? q.len - (end - q.q0) : 0;
   // (a length outside the table: one tile more than the table has, which is not there)
   const long long room = (long long)s.max_pages * s.page_tiles;
-  q.tiles = (int)max(1ll, min(((long long)q.len + kTile - 1) / kTile, room + 1));
+  q.units = ((int)max(1ll, min(((long long)q.len + kTile - 1) / kTile, room + 1)) + kTiles - 1) / kTiles;
   q.n_row_tiles = (int)(((long long)q.m * a.shared + kRows - 1) / kRows);
   return q;
 }
@@ -125,25 +135,27 @@ struct Pending {
   long long out[kMaxRows];
 };
 
-template <int G, int T, int NT>
+template <int G, int T, int L, int NT>
 __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a, Control* ctl) {
-  using C = Cfg<G, T, NT>;
-  constexpr int kLR = C::kLaneRows;
+  using C = Cfg<G, T, L, NT>;
+  constexpr int kLR = C::kLaneRows, N = C::kTiles;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ Scan2 s_warp[kWarps];
   __shared__ long long s_before[kThreads];   // units before a thread's sequences
   __shared__ Pending s_pending[kWarps * 2];
   __shared__ int s_n_pending;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gr = lane >> 2, t4 = lane & 3;
-  unsigned char* ring = smem + warp * C::kWarpBytes;
-  unsigned char* s_q = ring + C::kRing;
-  float* s_sum = reinterpret_cast<float*>(s_q + C::kQ);   // [G][kRows]
-  float* s_start = s_sum + G * C::kRows;                  // [G][kRows][2]
-  float* s_factor = s_start + 2 * G * C::kRows;           // [kRows]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(s_factor + C::kRows);
+  unsigned char* ring_k = smem + warp * C::kWarpBytes;
+  unsigned char* ring_v = ring_k + C::kRing / 2;
+  unsigned char* s_q = ring_k + C::kRing;
+  float* s_start = reinterpret_cast<float*>(s_q + C::kQ);   // [G][kRows][2]
+  float* s_sum = s_start + 2 * G * C::kRows;                // [G][kRows]
+  float* s_factor = s_sum + G * C::kRows;                   // [kRows]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(s_q + C::kQ + C::kSums);   // of K, then of V
+  auto load = [&](int i) { return load_seq<C::kRows, N>(s, a, i); };
 
   if (lane == 0)
-    for (int i = 0; i < C::kStages; ++i) mbar_init(bars + i, C::kBoth);
+    for (int i = 0; i < 2 * C::kStages; ++i) mbar_init(bars + i, N);
   for (int i = lane; i < (C::kQ + C::kSums) / 4; i += 32) reinterpret_cast<uint32_t*>(s_q)[i] = 0u;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   if (tid == 0) s_n_pending = 0;
@@ -152,19 +164,19 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
   const int per = (a.n_seqs + kThreads - 1) / kThreads;
   Scan2 sum{0, 0}, total;
   for (int i = tid * per; i < min(tid * per + per, a.n_seqs); ++i) {
-    const Seq x = load_seq<C::kRows>(s, a, i);
-    sum.a += x.segments(s) * x.tiles;
+    const Seq x = load(i);
+    sum.a += x.all(s);
     sum.b += x.segments(s);
   }
   s_before[tid] = block_scan(sum, &total, s_warp).a;
-  const long long shares = max(1ll, min((long long)kMaxShares, max(total.a / kSnap, total.b)));
+  const long long shares = max(1ll, min((long long)kMaxShares, max(total.a / C::kSnap, total.b)));
   const int share = warp * kGrid + blockIdx.x;   // (few shares: one a block)
   const bool any = total.a > 0 && share < shares;
   if (total.a == 0 || blockIdx.x >= shares) return;
   __syncthreads();
   // where a share begins: the unit, its sequence and that one's first unit
   auto begin_of = [&](int x_share, int* x_seq, long long* x_base) {
-    const long long x = total.a * x_share / shares;
+    const long long x = quotient(total.a * x_share, shares);
     if (x >= total.a) return total.a;
     int lo = 0, hi = kThreads;
     while (hi - lo > 1) {
@@ -174,15 +186,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
     }
     long long base = s_before[lo];
     int i = lo * per;
-    Seq q = load_seq<C::kRows>(s, a, i);
-    for (long long n; x >= base + (n = q.segments(s) * q.tiles);) {
+    Seq q = load(i);
+    for (long long n; x >= base + (n = q.all(s));) {
       base += n;
-      q = load_seq<C::kRows>(s, a, ++i);
+      q = load(++i);
     }
     *x_seq = i;
     *x_base = base;
-    const long long begin = base + (x - base) / q.tiles * q.tiles, from = x - begin, to = begin + q.tiles - x;
-    return from < kSnap && from <= to ? begin : to < kSnap ? begin + q.tiles : x;
+    const long long begin = base + quotient(x - base, q.units) * q.units, from = x - begin, to = begin + q.units - x;
+    return from < C::kSnap && from <= to ? begin : to < C::kSnap ? begin + q.units : x;
   };
 
   if (any) {
@@ -190,47 +202,38 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
     long long base = 0, skip_base;
     int skip_seq;
     const long long u0 = begin_of(share, &seq, &base), u1 = begin_of(share + 1, &skip_seq, &skip_base);
-    const int mine = (int)(u1 - u0);   // the warp's tiles
+    const int mine = (int)(u1 - u0);   // the warp's units
     Seq q;
-    int head = 0, row_tile = 0, tile = 0;   // of the next unit
+    int head = 0, row_tile = 0, unit = 0;   // of the next unit
     if (mine > 0) {
-      q = load_seq<C::kRows>(s, a, seq);
-      while (u0 >= base + q.segments(s) * q.tiles) {   // (the share begins where the sequence ended)
-        base += q.segments(s) * q.tiles;
-        q = load_seq<C::kRows>(s, a, ++seq);
+      q = load(seq);
+      while (u0 >= base + q.all(s)) {   // (the share begins where the sequence ended)
+        base += q.all(s);
+        q = load(++seq);
       }
-      const long long segment = (u0 - base) / q.tiles;
-      tile = (int)(u0 - base - segment * q.tiles);
-      head = (int)(segment / q.n_row_tiles);
+      const long long segment = quotient(u0 - base, q.units);
+      unit = (int)(u0 - base - segment * q.units);
+      head = (int)quotient(segment, q.n_row_tiles);
       row_tile = (int)(segment - (long long)head * q.n_row_tiles);
     }
 
-    // ---- its tiles come through a ring; lane j % 32 knows where tile j lies
+    // ---- its tiles come through two rings, K and V; lane (N j + i) % 32 knows where tile i of unit j lies
     int look_seq = seq;
     long long look_base = base;
     const unsigned char* where = nullptr;
     unsigned bad_even = 0u, bad_odd = 0u;   // tiles without a page, of batches of 32
     auto look_up = [&](int batch) {
-      const long long u = u0 + batch * 32 + lane;
+      const long long u = u0 + batch * (32 / N) + lane / N;
       bool wrong = false;
       where = nullptr;
       if (u < u1) {
-        Seq x = load_seq<C::kRows>(s, a, look_seq);
-        for (long long n; u >= look_base + (n = x.segments(s) * x.tiles);) {
+        Seq x = load(look_seq);
+        for (long long n; u >= look_base + (n = x.all(s));) {
           look_base += n;
-          x = load_seq<C::kRows>(s, a, ++look_seq);
+          x = load(++look_seq);
         }
-        const long long local = u - look_base;
-        int at, of;
-        if (local >> 31) {
-          const long long segment = local / x.tiles;
-          at = (int)(local - segment * x.tiles);
-          of = (int)(segment / x.n_row_tiles);
-        } else {
-          const unsigned segment = (unsigned)local / (unsigned)x.tiles;
-          at = (int)((unsigned)local - segment * (unsigned)x.tiles);
-          of = (int)(segment / (unsigned)x.n_row_tiles);
-        }
+        const long long local = u - look_base, segment = quotient(local, x.units);
+        const int at = (int)(local - segment * x.units) * N + lane % N, of = (int)quotient(segment, x.n_row_tiles);
         if ((long long)at * kTile < x.len) {
           const int index = at / s.page_tiles;
           const int page = index < s.max_pages ? __ldg(a.table + (long long)look_seq * s.max_pages + index) : -1;
@@ -242,47 +245,43 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       if (batch & 1) bad_odd = mask;
       else bad_even = mask;
     };
-    int issued = 0, to_stage = 0;   // tiles, a stage's at a time
-    auto issue = [&]() {
-      if (issued >= mine) return;
-      if ((issued & 31) == 0) look_up(issued >> 5);
-      if ((lane & -C::kBoth) == (issued & 31)) {
+    // K (V) of unit j, if there is one, to its stage
+    auto issue = [&](int j, int stage, bool of_v) {
+      if (j >= mine) return;
+      if (!of_v && j % (32 / N) == 0) look_up(j / (32 / N));
+      if (lane / N == j % (32 / N)) {
+        uint64_t* bar = bars + (of_v ? C::kStages : 0) + stage;
         if (where) {
-          mbar_expect_tx(bars + to_stage, C::kTileBytes);
-          copy_tile(s32(ring) + (to_stage * C::kBoth + (lane & (C::kBoth - 1))) * C::kTileBytes, where, C::kTileBytes, bars + to_stage);
+          mbar_expect_tx(bar, C::kHalf);
+          copy_tile(s32(of_v ? ring_v : ring_k) + (stage * N + lane % N) * C::kHalf, where + (of_v ? C::kHalf : 0), C::kHalf, bar);
         } else {
-          mbar_arrive(bars + to_stage);
+          mbar_arrive(bar);
         }
       }
-      issued += C::kBoth;
-      if (++to_stage == C::kStages) to_stage = 0;
     };
-    for (int i = 0; i < C::kStages; ++i) issue();
-
+    for (int i = 0; i < C::kStages; ++i) {
+      issue(i, i, false);
+      issue(i, i, true);
+    }
     int stage = 0;
     uint32_t phase = 0;
     bool gave_up = false;    // a copy did not arrive
-    const unsigned char* at = ring;   // the stage that has arrived
-    // Tile j (the next): waits where it is the first of a stage.
-    auto arrive = [&](int j) {
-      if (j & (C::kBoth - 1)) return;
-      if (__any_sync(0xffffffffu, !mbar_wait(bars + stage, phase))) gave_up = true;
-      at = ring + stage * C::kBoth * C::kTileBytes;
-    };
-    // Tiles before j are read: the stage goes back where they were its last.
-    auto hand_back = [&](int j) {
-      if (j & (C::kBoth - 1)) return;
-      __syncwarp();
-      issue();
-      if (++stage == C::kStages) {
-        stage = 0;
-        phase ^= 1u;
-      }
-    };
+
+    // what of the columns' operands is of tile i: the columns of the others are zero
+    uint32_t only[N];
+    const unsigned char* q_at[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool of = gr / (2 * L) == i;
+      only[i] = of ? ~0u : 0u;
+      q_at[i] = s_q + ((N == 1 || of ? gr % (2 * L) : 2 * L) * 4 + t4) * 16;
+    }
+    const int my_tile = t4 / L;   // the one whose scores this lane has
+    auto row_of = [&](int n, int r) { return T == 2 ? n * L + t4 % L : n * 2 * L + t4 % L * 2 + r; };
 
     // ---- segments of the share
     for (int j = 0; j < mine && !gave_up;) {
-      const int n_tiles = min(q.tiles - tile, mine - j);   // of this segment
+      const int n_units = min(q.units - unit, mine - j);   // of this segment
       const int row0 = row_tile * C::kRows, n_rows = min(C::kRows, q.m * a.shared - row0);
       // row r of the tile: row of the step, q head; its tokens
       auto step_row = [&](int r) { return (row0 + r) / a.shared; };
@@ -305,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
         int k = (T == 2 ? 137 : 140) - (int)(__float_as_uint(top) >> 23);
         if (top == 0.f || top > 3.402823466e38f) k = 0;
         const float k0 = __uint_as_float((uint32_t)(127 + k / 2) << 23), k1 = __uint_as_float((uint32_t)(127 + k - k / 2) << 23);
-        float part[G], first[G];   // sums of q 2^k and of its first term
+        float part[G], first[G];   // sums of q 2^k (T = 2: of its second term) and of its first term
 #pragma unroll
         for (int g = 0; g < G; ++g) part[g] = first[g] = 0.f;
 #pragma unroll
@@ -316,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
           part[g] += T == 2 ? lo : x;
           first[g] += hi;
           // word (c % 16) / 8 of lane c / 16: its two steps' registers (nib / 2) % 2, b0 or b1 nib % 2, half nib / 4
-          const int col = T == 2 ? (r & 3) * 2 : r & 7, nt = T == 2 ? r >> 2 : r >> 3;
+          const int col = T == 2 ? r % L * 2 : r % (2 * L), nt = T == 2 ? r / L : r / (2 * L);
           __half* to = reinterpret_cast<__half*>(s_q + ((nt * G + g) * 2 + (c % 16) / 8) * 512 + (col * 4 + c / 16) * 16) + (nib / 2 % 2) * 4 +
                        (nib & 1) * 2 + nib / 4;
           *to = __float2half_rn(hi * odd);
@@ -336,10 +335,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       }
       __syncwarp();
 
+      // sums and maxima, of each tile of a unit its own until the segment ends
       float O[NT][G][4][4], z[NT][kLR][G], m[NT][kLR], l[NT][kLR], m_flush[NT], factor[NT][kLR];
       float vs = 0.f, vinv = 0.f;   // a power of two not below any s of V so far, and kOne / vs
       bool flushed = false;
-      auto row_of = [&](int n, int r) { return T == 2 ? n * 4 + t4 : n * 8 + t4 * 2 + r; };
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -360,85 +359,93 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       }
       const int least = sees(0), most = sees(n_rows - 1);
 
-      // N tiles; masked: one that some row does not see all of, or without a page
-      auto pass = [&](auto tiles, auto is_masked, const unsigned char* first, int pos, bool wrong) {
-        constexpr int N = decltype(tiles)::value;
+      // A unit from token `first_pos` on; masked: where some row does not see all of it, or a page is missing (a bit for each tile)
+      auto pass = [&](auto is_masked, int first_pos, unsigned missing, int next) {
         constexpr bool kMasked = decltype(is_masked)::value;
-        float S[N][NT][kLR][2];
-        uint2 pv[N][G];
-        __half2 steps = __half2half2(__ushort_as_half(0));
+        const int pos = first_pos + my_tile * kTile + gr;
+        const bool wrong = kMasked && (missing >> my_tile & 1u);
+        float S[NT][kLR][2], p[NT][kLR][2];
+        const unsigned char* k_at = ring_k + stage * N * C::kHalf;
+        const unsigned char* v_at = ring_v + stage * N * C::kHalf;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const unsigned char* at = first + i * C::kTileBytes;
+        for (int g = 0; g < G; ++g) {
+          const uint2 pw = reinterpret_cast<const uint2*>(k_at + my_tile * C::kHalf + g * kBlockBytes + kCodeBytes)[gr];
+          float acc[NT][4];
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
-            const uint4 w = reinterpret_cast<const uint4*>(at + g * kBlockBytes)[lane];
-            const uint2 pw = reinterpret_cast<const uint2*>(at + g * kBlockBytes + kCodeBytes)[gr];
-            float acc[NT][4];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              // -8 times the sum of the column's q: the sums are those of code - 8
-              if constexpr (T == 2) {
-                const float2 v = reinterpret_cast<const float2*>(s_start)[g * C::kRows + n * 4 + t4];
-                acc[n][0] = acc[n][2] = v.x;
-                acc[n][1] = acc[n][3] = v.y;
-              } else {
-                const float4 v = reinterpret_cast<const float4*>(s_start)[(g * C::kRows + n * 8) / 2 + t4];
-                acc[n][0] = acc[n][2] = v.x;
-                acc[n][1] = acc[n][3] = v.z;
-              }
+          for (int n = 0; n < NT; ++n) {
+            // -8 times the sum of the column's q: the sums are those of code - 8
+            if constexpr (T == 2) {
+              const float2 v = reinterpret_cast<const float2*>(s_start)[g * C::kRows + row_of(n, 0)];
+              acc[n][0] = acc[n][2] = v.x;
+              acc[n][1] = acc[n][3] = v.y;
+            } else {
+              const float4 v = reinterpret_cast<const float4*>(s_start)[(g * C::kRows + row_of(n, 0)) / 2];
+              acc[n][0] = acc[n][2] = v.x;
+              acc[n][1] = acc[n][3] = v.z;
             }
+          }
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const uint4 w = reinterpret_cast<const uint4*>(k_at + i * C::kHalf + g * kBlockBytes)[lane];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const uint32_t x = h ? w.y : w.x, y = h ? w.w : w.z;
               const uint32_t x8 = x >> 8, y8 = y >> 8;
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
-                const uint4 bq = reinterpret_cast<const uint4*>(s_q + ((n * G + g) * 2 + h) * 512)[lane];
+                const uint4 bq = *reinterpret_cast<const uint4*>(q_at[i] + ((n * G + g) * 2 + h) * 512);
                 mma_f16(acc[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, bq.x, bq.y);
                 mma_f16(acc[n], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, bq.z, bq.w);
               }
             }
-            const float2 p0 = unpack_half2(pw.x), p1 = unpack_half2(pw.y);   // (s, mid) of tokens gr and gr + 8
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int r = 0; r < kLR; ++r) {
-                const float qs = s_sum[g * C::kRows + row_of(n, r)];
-                const float a0 = T == 2 ? fmaf(acc[n][1], 1.f / kLow, acc[n][0]) : acc[n][r];
-                const float a1 = T == 2 ? fmaf(acc[n][3], 1.f / kLow, acc[n][2]) : acc[n][2 + r];
-                S[i][n][r][0] = fmaf(p0.x, a0, g ? fmaf(p0.y, qs, S[i][n][r][0]) : p0.y * qs);
-                S[i][n][r][1] = fmaf(p1.x, a1, g ? fmaf(p1.y, qs, S[i][n][r][1]) : p1.y * qs);
-              }
-            // pairs of V, and their largest step
-            pv[i][g] = reinterpret_cast<const uint2*>(at + (G + g) * kBlockBytes + kCodeBytes)[gr];
-            if constexpr (kMasked) {   // (behind the last token lies anything)
-              if (wrong || pos + gr >= q.len) pv[i][g].x = 0u;
-              if (wrong || pos + gr + 8 >= q.len) pv[i][g].y = 0u;
-            }
-            steps = __hmax2(steps, __hmax2(*reinterpret_cast<const __half2*>(&pv[i][g].x), *reinterpret_cast<const __half2*>(&pv[i][g].y)));
           }
-        }
-        const float step = __low2float(steps);
-        bool move = step > vs;
-        float p[N][NT][kLR][2];
-#pragma unroll
-        for (int i = 0; i < N; ++i)
+          const float2 p0 = unpack_half2(pw.x), p1 = unpack_half2(pw.y);   // (s, mid) of tokens gr and gr + 8
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < kLR; ++r) {
-              if constexpr (kMasked) {
-                const int vis = sees(row_of(n, r)) - pos - gr;
-                S[i][n][r][0] = vis <= 0 ? -INFINITY : wrong ? NAN : S[i][n][r][0];
-                S[i][n][r][1] = vis <= 8 ? -INFINITY : wrong ? NAN : S[i][n][r][1];
-              }
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                p[i][n][r][e] = fmaf(S[i][n][r][e], factor[n][r], -m[n][r]);
-                move = move || p[i][n][r][e] > kLazy;
-              }
+              const float qs = s_sum[g * C::kRows + row_of(n, r)];
+              const float a0 = T == 2 ? fmaf(acc[n][1], 1.f / kLow, acc[n][0]) : acc[n][r];
+              const float a1 = T == 2 ? fmaf(acc[n][3], 1.f / kLow, acc[n][2]) : acc[n][2 + r];
+              S[n][r][0] = fmaf(p0.x, a0, g ? fmaf(p0.y, qs, S[n][r][0]) : p0.y * qs);
+              S[n][r][1] = fmaf(p1.x, a1, g ? fmaf(p1.y, qs, S[n][r][1]) : p1.y * qs);
             }
+        }
+        __syncwarp();
+        issue(next, stage, false);
+        if (__any_sync(0xffffffffu, !mbar_wait(bars + C::kStages + stage, phase))) {
+          gave_up = true;
+          return;
+        }
+        // pairs of V, and their largest step
+        uint2 pv[G];
+        __half2 steps = __half2half2(__ushort_as_half(0));
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          pv[g] = reinterpret_cast<const uint2*>(v_at + my_tile * C::kHalf + g * kBlockBytes + kCodeBytes)[gr];
+          if constexpr (kMasked) {   // (behind the last token lies anything)
+            if (wrong || pos >= q.len) pv[g].x = 0u;
+            if (wrong || pos + 8 >= q.len) pv[g].y = 0u;
+          }
+          steps = __hmax2(steps, __hmax2(*reinterpret_cast<const __half2*>(&pv[g].x), *reinterpret_cast<const __half2*>(&pv[g].y)));
+        }
+        const float step = __low2float(steps);
+        bool move = step > vs;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < kLR; ++r) {
+            if constexpr (kMasked) {
+              const int vis = sees(row_of(n, r)) - pos;
+              S[n][r][0] = vis <= 0 ? -INFINITY : wrong ? NAN : S[n][r][0];
+              S[n][r][1] = vis <= 8 ? -INFINITY : wrong ? NAN : S[n][r][1];
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              p[n][r][e] = fmaf(S[n][r][e], factor[n][r], -m[n][r]);
+              move = move || p[n][r][e] > kLazy;
+            }
+          }
         if (__any_sync(0xffffffffu, move)) {
           float largest = step;
 #pragma unroll
@@ -452,9 +459,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < kLR; ++r) {
-              float x = m[n][r];
-#pragma unroll
-              for (int i = 0; i < N; ++i) x = fmaxf(x, fmaxf(S[i][n][r][0] * factor[n][r], S[i][n][r][1] * factor[n][r]));
+              float x = fmaxf(m[n][r], fmaxf(S[n][r][0] * factor[n][r], S[n][r][1] * factor[n][r]));
 #pragma unroll
               for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
               if (x - m[n][r] <= kLazy) x = m[n][r];   // (another row's: this one's sums stay as they are)
@@ -465,9 +470,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
               for (int g = 0; g < G; ++g) z[n][r][g] *= keep[n][r];
               keep[n][r] *= v_keep;
 #pragma unroll
-              for (int i = 0; i < N; ++i)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) p[i][n][r][e] = fmaf(S[i][n][r][e], factor[n][r], -x);
+              for (int e = 0; e < 2; ++e) p[n][r][e] = fmaf(S[n][r][e], factor[n][r], -x);
             }
 #pragma unroll
           for (int n = 0; n < NT; ++n)
@@ -478,68 +481,69 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
 #pragma unroll
                 for (int e = 0; e < 4; ++e) O[n][g][i][e] *= keep[n][kLR == 2 ? e & 1 : 0];
         }
+        float ps[NT][kLR][2];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const unsigned char* at = first + i * C::kTileBytes + G * kBlockBytes;
-          float ps[NT][kLR][2];
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+          for (int r = 0; r < kLR; ++r)
 #pragma unroll
-            for (int r = 0; r < kLR; ++r)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                p[i][n][r][e] = exp2_fast(p[i][n][r][e]);
-                l[n][r] += p[i][n][r][e];
-                ps[n][r][e] = p[i][n][r][e] * vinv;
-              }
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            const uint4 w = reinterpret_cast<const uint4*>(at + g * kBlockBytes)[lane];
-            const float2 p0 = unpack_half2(pv[i][g].x), p1 = unpack_half2(pv[i][g].y);
-            uint32_t b0[NT], b1[NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              float x[kLR][2];
-#pragma unroll
-              for (int r = 0; r < kLR; ++r) {
-                x[r][0] = ps[n][r][0] * p0.x;
-                x[r][1] = ps[n][r][1] * p1.x;
-                if constexpr (kMasked) {   // (a token that this row does not see need not be a number)
-                  const int vis = sees(row_of(n, r)) - pos - gr;
-                  if (vis <= 0) x[r][0] = 0.f;
-                  else z[n][r][g] = fmaf(p[i][n][r][0], p0.y, z[n][r][g]);
-                  if (vis <= 8) x[r][1] = 0.f;
-                  else z[n][r][g] = fmaf(p[i][n][r][1], p1.y, z[n][r][g]);
-                } else {
-                  z[n][r][g] = fmaf(p[i][n][r][1], p1.y, fmaf(p[i][n][r][0], p0.y, z[n][r][g]));
-                }
-              }
-              if constexpr (T == 2) {   // its upper eleven bits and the rest
-                const float h0 = __uint_as_float(__float_as_uint(x[0][0]) & 0xFFFFE000u), h1 = __uint_as_float(__float_as_uint(x[0][1]) & 0xFFFFE000u);
-                b0[n] = pack_half2(h0, x[0][0] - h0);
-                b1[n] = pack_half2(h1, x[0][1] - h1);
-              } else {
-                b0[n] = pack_half2(x[0][0], x[kLR - 1][0]);
-                b1[n] = pack_half2(x[0][1], x[kLR - 1][1]);
-              }
-              b0[n] = transpose8x8(b0[n]);
-              b1[n] = transpose8x8(b1[n]);
+            for (int e = 0; e < 2; ++e) {
+              p[n][r][e] = exp2_fast(p[n][r][e]);
+              l[n][r] += p[n][r][e];
+              ps[n][r][e] = p[n][r][e] * vinv;
             }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const float2 p0 = unpack_half2(pv[g].x), p1 = unpack_half2(pv[g].y);
+          uint32_t b0[NT], b1[NT];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float x[kLR][2];
+#pragma unroll
+            for (int r = 0; r < kLR; ++r) {
+              x[r][0] = ps[n][r][0] * p0.x;
+              x[r][1] = ps[n][r][1] * p1.x;
+              if constexpr (kMasked) {   // (a token that this row does not see need not be a number)
+                const int vis = sees(row_of(n, r)) - pos;
+                if (vis <= 0) x[r][0] = 0.f;
+                else z[n][r][g] = fmaf(p[n][r][0], p0.y, z[n][r][g]);
+                if (vis <= 8) x[r][1] = 0.f;
+                else z[n][r][g] = fmaf(p[n][r][1], p1.y, z[n][r][g]);
+              } else {
+                z[n][r][g] = fmaf(p[n][r][1], p1.y, fmaf(p[n][r][0], p0.y, z[n][r][g]));
+              }
+            }
+            if constexpr (T == 2) {   // its upper eleven bits and the rest
+              const float h0 = __uint_as_float(__float_as_uint(x[0][0]) & 0xFFFFE000u), h1 = __uint_as_float(__float_as_uint(x[0][1]) & 0xFFFFE000u);
+              b0[n] = pack_half2(h0, x[0][0] - h0);
+              b1[n] = pack_half2(h1, x[0][1] - h1);
+            } else {
+              b0[n] = pack_half2(x[0][0], x[kLR - 1][0]);
+              b1[n] = pack_half2(x[0][1], x[kLR - 1][1]);
+            }
+            b0[n] = transpose8x8(b0[n]);
+            b1[n] = transpose8x8(b1[n]);
+          }
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const uint4 w = reinterpret_cast<const uint4*>(v_at + i * C::kHalf + g * kBlockBytes)[lane];
             const uint32_t x8 = w.x >> 8, y8 = w.y >> 8, z8 = w.z >> 8, w8 = w.w >> 8;
             const uint32_t A[4][4] = {{centred<false>(w.x), centred<false>(w.y), centred<false>(w.z), centred<false>(w.w)},
                                       {centred<true>(w.x), centred<true>(w.y), centred<true>(w.z), centred<true>(w.w)},
                                       {centred<false>(x8), centred<false>(y8), centred<false>(z8), centred<false>(w8)},
                                       {centred<true>(x8), centred<true>(y8), centred<true>(z8), centred<true>(w8)}};
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int n = 0; n < NT; ++n) {
+              const uint32_t c0 = N == 1 ? b0[n] : b0[n] & only[i], c1 = N == 1 ? b1[n] : b1[n] & only[i];
 #pragma unroll
-              for (int n = 0; n < NT; ++n) mma_f16(O[n][g][k], A[k][0], A[k][1], A[k][2], A[k][3], b0[n], b1[n]);
+              for (int k = 0; k < 4; ++k) mma_f16(O[n][g][k], A[k][0], A[k][1], A[k][2], A[k][3], c0, c1);
+            }
           }
         }
       };
 
       // the warp's part of a segment that it shares (or that it has to sum in pieces): channels 8 gr .. + 7 of a block
-      const bool tail = tile == 0;
+      const bool tail = unit == 0;
       float* part = a.parts + (2ll * share + tail) * C::kPart;
       auto lane_sums = [&](int n, int g, int r, float (&v)[8]) {
         const float f = vs * (1.f / kOne);
@@ -550,43 +554,42 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
         }
         if (T == 2 && flushed) {
           const float keep = exp2_fast(m_flush[n] - m[n][r]);
-          const float4* from = reinterpret_cast<const float4*>(part + row_of(n, r) * C::kDim + g * kGroup + gr * 8);
+          const float4* from = reinterpret_cast<const float4*>(part + (n * 4 + t4) * C::kDim + g * kGroup + gr * 8);
           const float4 x = __ldcg(from), y = __ldcg(from + 1);
           v[0] = fmaf(x.x, keep, v[0]), v[1] = fmaf(x.y, keep, v[1]), v[2] = fmaf(x.z, keep, v[2]), v[3] = fmaf(x.w, keep, v[3]);
           v[4] = fmaf(y.x, keep, v[4]), v[5] = fmaf(y.y, keep, v[5]), v[6] = fmaf(y.z, keep, v[6]), v[7] = fmaf(y.w, keep, v[7]);
         }
       };
-      auto to_part = [&](int n, int g, int r, const float (&v)[8]) {
-        float4* to = reinterpret_cast<float4*>(part + row_of(n, r) * C::kDim + g * kGroup + gr * 8);
+      auto to_part = [&](int row, int g, const float (&v)[8]) {
+        float4* to = reinterpret_cast<float4*>(part + row * C::kDim + g * kGroup + gr * 8);
         __stcg(to, make_float4(v[0], v[1], v[2], v[3]));
         __stcg(to + 1, make_float4(v[4], v[5], v[6], v[7]));
       };
 
-      const int end = j + n_tiles;
+      const int end = j + n_units;
       int since = 0;
-      for (int pos = tile * kTile; j < end;) {
-        arrive(j);
+      for (int pos = unit * N * kTile; j < end; pos += N * kTile) {
+        if (__any_sync(0xffffffffu, !mbar_wait(bars + stage, phase))) gave_up = true;
         if (gave_up) break;
-        const unsigned missing = ((j & 32) ? bad_odd : bad_even) >> (j & 31);   // tiles from j on that have no page
-        if (C::kPair == 2 && !(j & 1) && j + 1 < end && least - pos >= 2 * kTile && !(missing & 3u)) {
-          pass(std::integral_constant<int, C::kPair>{}, std::false_type{}, at, pos, false);
-          j += 2;
-          pos += 2 * kTile;
-          since += 2;
+        const unsigned missing = ((j & 32 / N) ? bad_odd : bad_even) >> j % (32 / N) * N & ((1u << N) - 1);   // tiles that have no page
+        if (missing && lane == 0) ctl->status = GSI_ERR_INVALID_ARG;
+        if (least - pos >= N * kTile && !missing) {
+          pass(std::false_type{}, pos, 0u, j + C::kStages);
+        } else if (pos < most) {
+          pass(std::true_type{}, pos, missing, j + C::kStages);
         } else {
-          if (pos < most) {
-            const bool wrong = missing & 1u;
-            if (wrong && lane == 0) ctl->status = GSI_ERR_INVALID_ARG;
-            const unsigned char* one = at + (j & (C::kBoth - 1)) * C::kTileBytes;
-            if (C::kPair == 1 && least - pos >= kTile && !wrong) pass(std::integral_constant<int, 1>{}, std::false_type{}, one, pos, false);
-            else pass(std::integral_constant<int, 1>{}, std::true_type{}, one, pos, wrong);
-            ++since;
-          }
-          ++j;
-          pos += kTile;
+          issue(j + C::kStages, stage, false);
+          if (__any_sync(0xffffffffu, !mbar_wait(bars + C::kStages + stage, phase))) gave_up = true;
         }
-        hand_back(j);
-        if (T == 2 && since >= kFlush && j < end) {
+        if (gave_up) break;
+        __syncwarp();
+        issue(j + C::kStages, stage, true);
+        if (++stage == C::kStages) {
+          stage = 0;
+          phase ^= 1u;
+        }
+        ++j;
+        if (T == 2 && ++since == kFlush && j < end) {
           since = 0;
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
@@ -594,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
             for (int g = 0; g < G; ++g) {
               float v[8];
               lane_sums(n, g, 0, v);
-              to_part(n, g, 0, v);
+              to_part(n * 4 + t4, g, v);
 #pragma unroll
               for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -613,28 +616,36 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
           for (int r = 0; r < kLR; ++r) l[n][r] = NAN;
       }
 
-      // ---- the segment's sums: out, where they are the whole of it
-      const bool whole = tail && n_tiles == q.tiles;
+      // ---- the segment's sums: over the lanes and the tiles of a unit; out, where they are the whole of it
+      const bool whole = tail && n_units == q.units;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int r = 0; r < kLR; ++r) {
+          float top = m[n][r];
 #pragma unroll
-          for (int o = 4; o < 32; o <<= 1) {
-            l[n][r] += __shfl_xor_sync(0xffffffffu, l[n][r], o);
+          for (int o = L; o < 4; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const float share_of = exp2_fast(m[n][r] - top);
+          l[n][r] *= share_of;
 #pragma unroll
-            for (int g = 0; g < G; ++g) z[n][r][g] += __shfl_xor_sync(0xffffffffu, z[n][r][g], o);
-          }
+          for (int o = L; o < 32; o <<= 1) l[n][r] += __shfl_xor_sync(0xffffffffu, l[n][r], o);
           const int row = row_of(n, r);
-          if (row >= n_rows) continue;
+          const bool writes = t4 < L && row < n_rows;
           const long long to = (long long)(q.q0 + step_row(row)) * a.out_token + q_head(row) * a.out_head;
           const float over = l[n][r] == 0.f ? 0.f : 1.f / l[n][r];   // (no token seen: 0)
 #pragma unroll
           for (int g = 0; g < G; ++g) {
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) z[n][r][g] += __shfl_xor_sync(0xffffffffu, z[n][r][g], o);
             float v[8];
             lane_sums(n, g, r, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += z[n][r][g];
+            for (int i = 0; i < 8; ++i) {
+              v[i] = (v[i] + z[n][r][g]) * share_of;
+#pragma unroll
+              for (int o = L; o < 4; o <<= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+            }
+            if (!writes) continue;
             if (whole) {
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
@@ -642,41 +653,38 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
                 if (c < s.head_dim) store_from_float(a.out, a.dtype, to + c, v[i] * over);
               }
             } else {
-              to_part(n, g, r, v);
+              to_part(row, g, v);
             }
           }
-          if (!whole && gr == 0) __stcg(reinterpret_cast<float2*>(part + C::kRows * C::kDim) + row, make_float2(m[n][r], l[n][r]));
+          if (!whole && writes && gr == 0) __stcg(reinterpret_cast<float2*>(part + C::kPartRows * C::kDim) + row, make_float2(top, l[n][r]));
         }
       if (!whole) {
         // the boundaries between shares that lie within the segment: shares first .. first + n_parts - 1 have a part
-        const long long begin = u0 + (end - n_tiles) - tile, behind = begin + q.tiles;   // (end: of the piece, in tiles of the share)
-        const long long b1 = ((begin + kSnap) * shares + total.a - 1) / total.a, b2 = ((behind - kSnap + 1) * shares + total.a - 1) / total.a - 1;
+        const long long begin = u0 + (end - n_units) - unit, behind = begin + q.units;
+        const long long b1 = quotient((begin + C::kSnap) * shares + total.a - 1, total.a);
+        const long long b2 = quotient((behind - C::kSnap + 1) * shares + total.a - 1, total.a) - 1;
         const int first = (int)b1 - 1, n_parts = (int)(b2 - b1) + 2;
         __threadfence();
         __syncwarp();
-        bool last = false;
-        if (lane == 0) {
-          last = atomicAdd(a.tickets + first, 1u) == (unsigned)n_parts - 1;
-          if (last) {
-            a.tickets[first] = 0u;
-            __threadfence();
-            Pending& x = s_pending[atomicAdd(&s_n_pending, 1)];
-            x.first = first;
-            x.parts = n_parts;
-            x.rows = n_rows;
-            for (int r = 0; r < n_rows; ++r) x.out[r] = (long long)(q.q0 + step_row(r)) * a.out_token + q_head(r) * a.out_head;
-          }
+        if (lane == 0 && atomicAdd(a.tickets + first, 1u) == (unsigned)n_parts - 1) {
+          a.tickets[first] = 0u;
+          __threadfence();
+          Pending& x = s_pending[atomicAdd(&s_n_pending, 1)];
+          x.first = first;
+          x.parts = n_parts;
+          x.rows = n_rows;
+          for (int r = 0; r < n_rows; ++r) x.out[r] = (long long)(q.q0 + step_row(r)) * a.out_token + q_head(r) * a.out_head;
         }
       }
       // the next segment
-      tile += n_tiles;
-      if (tile == q.tiles) {
-        tile = 0;
+      unit += n_units;
+      if (unit == q.units) {
+        unit = 0;
         if (++row_tile == q.n_row_tiles) {
           row_tile = 0;
           if (++head == s.n_heads) {
             head = 0;
-            if (end < mine) do q = load_seq<C::kRows>(s, a, ++seq);
+            if (end < mine) do q = load(++seq);
               while (q.n_row_tiles == 0);
           }
         }
@@ -686,6 +694,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       // (copies in flight land before the block's memory is another's)
       for (int i = 0; i < C::kStages; ++i) {
         mbar_wait(bars + stage, phase);
+        mbar_wait(bars + C::kStages + stage, phase);
         if (++stage == C::kStages) {
           stage = 0;
           phase ^= 1u;
@@ -714,7 +723,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
           for (int y = 0; y < 4; ++y) {
             const int b = min(y0 + y * kSets, x.parts - 1);
             const float* from = a.parts + (2ll * (x.first + b) + (b == 0)) * C::kPart;
-            ml[y] = __ldcg(reinterpret_cast<const float2*>(from + C::kRows * C::kDim) + r);
+            ml[y] = __ldcg(reinterpret_cast<const float2*>(from + C::kPartRows * C::kDim) + r);
             px[y] = __ldcg(reinterpret_cast<const float4*>(from + r * C::kDim) + c4);
           }
 #pragma unroll
@@ -749,54 +758,57 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
   }
 }
 
-template <int G, int T, int NT>
+template <int G, int T, int L, int NT>
 cudaError_t launch(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
-  using C = Cfg<G, T, NT>;
+  using C = Cfg<G, T, L, NT>;
   static_assert(C::kSmem + 5120 <= 115712, "two blocks of an SM, with what else they hold in shared memory");
-  static_assert(C::kRows <= kMaxRows && C::kTileBytes % 16 == 0 && C::kSums % 16 == 0 && C::kPart <= kPartFloats(G), "layout");
-  if (!a.q) return cudaFuncSetAttribute(k_kv_attend<G, T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
-  k_kv_attend<G, T, NT><<<kGrid, kThreads, C::kSmem, stream>>>(s, a, ctl);
+  static_assert(C::kRows <= C::kPartRows && 4 * NT <= C::kPartRows && C::kHalf % 16 == 0 && C::kStages >= 1, "layout");
+  if (!a.q) return cudaFuncSetAttribute(k_kv_attend<G, T, L, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  k_kv_attend<G, T, L, NT><<<kGrid, kThreads, C::kSmem, stream>>>(s, a, ctl);
   return cudaGetLastError();
 }
 
-}  // namespace
-
-namespace {
-
-cudaError_t launch_of(int groups, bool two, bool wide, const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
-  switch (groups * 4 + two * 2 + wide) {
-    case 4: return launch<1, 1, 1>(s, a, ctl, stream);
-    case 5: return launch<1, 1, 2>(s, a, ctl, stream);
-    case 6: return launch<1, 2, 1>(s, a, ctl, stream);
-    case 7: return launch<1, 2, 2>(s, a, ctl, stream);
-    case 8: return launch<2, 1, 1>(s, a, ctl, stream);
-    case 9: return launch<2, 1, 2>(s, a, ctl, stream);
-    case 10: return launch<2, 2, 1>(s, a, ctl, stream);
-    case 11: return launch<2, 2, 2>(s, a, ctl, stream);
-    case 12: return launch<3, 1, 1>(s, a, ctl, stream);
-    case 14: return launch<3, 2, 1>(s, a, ctl, stream);
-    case 16: return launch<4, 1, 1>(s, a, ctl, stream);
-    case 18: return launch<4, 2, 1>(s, a, ctl, stream);
-    default: return cudaErrorInvalidValue;
+// `rows`: of a unit, in column pairs (1, 2, 4, or 8 in two column tiles)
+template <int G, int T>
+cudaError_t launch_rows(int rows, const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
+  if constexpr (G <= 2) {
+    if (rows == 1) return launch<G, T, 1, 1>(s, a, ctl, stream);
+    if (rows == 8) return launch<G, T, 4, 2>(s, a, ctl, stream);
+  }
+  if (rows <= 2) return launch<G, T, 2, 1>(s, a, ctl, stream);
+  return launch<G, T, 4, 1>(s, a, ctl, stream);
+}
+cudaError_t launch_any(bool two, int rows, const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
+  switch (s.groups * 2 + two) {
+    case 2: return launch_rows<1, 1>(rows, s, a, ctl, stream);
+    case 3: return launch_rows<1, 2>(rows, s, a, ctl, stream);
+    case 4: return launch_rows<2, 1>(rows, s, a, ctl, stream);
+    case 5: return launch_rows<2, 2>(rows, s, a, ctl, stream);
+    case 6: return launch_rows<3, 1>(rows, s, a, ctl, stream);
+    case 7: return launch_rows<3, 2>(rows, s, a, ctl, stream);
+    case 8: return launch_rows<4, 1>(rows, s, a, ctl, stream);
+    default: return launch_rows<4, 2>(rows, s, a, ctl, stream);
   }
 }
 
 }  // namespace
 
 cudaError_t prepare_attend(const Shape& s) {
-  for (int i = 0; i < (s.groups <= 2 ? 4 : 2); ++i) {
-    const bool wide = i >= 2;
-    const cudaError_t e = launch_of(s.groups, i & 1, wide, s, AttendArgs{}, nullptr, nullptr);
+  for (int i = 0; i < 8; ++i) {
+    const cudaError_t e = launch_any(i & 1, 1 << i / 2, s, AttendArgs{}, nullptr, nullptr);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
 
 cudaError_t launch_attend(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
-  // Rows of one column tile, or of two where sequences bring more on average and the registers have room for their sums.
+  // The smallest unit that holds the rows of a sequence on average (half a row left over may go to a second tile of rows:
+  // batches are padded).
   const bool two = a.dtype == GSI_F32;
-  const bool wide = s.groups <= 2 && (long long)a.n_rows * a.shared > (two ? 4ll : 8ll) * a.n_seqs;
-  return launch_of(s.groups, two, wide, s, a, ctl, stream);
+  const double mean = (double)a.n_rows * a.shared / a.n_seqs - 0.5;
+  int rows = 1;
+  while (rows < 8 && rows * (two ? 1 : 2) < mean) rows *= 2;
+  return launch_any(two, rows, s, a, ctl, stream);
 }
 
 }  // namespace kv
