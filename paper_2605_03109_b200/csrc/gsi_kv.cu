@@ -556,7 +556,7 @@ gsi_status_t gsi_kv_attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t
   if (!h || !is_type(dtype) || n_rows < 0 || n_q_heads <= 0 || n_q_heads % h->shape.n_heads || n_seqs <= 0 || n_seqs > h->shape.max_seqs ||
       !std::isfinite(scale))
     return GSI_ERR_INVALID_ARG;
-  if ((long long)n_rows * (n_q_heads / h->shape.n_heads) >= 1ll << 31) return GSI_ERR_UNSUPPORTED;
+  if ((long long)n_rows * n_q_heads >= 1ll << 31) return GSI_ERR_UNSUPPORTED;
   if (n_rows == 0) return GSI_OK;
   if (!aligned(q, size_of(dtype)) || !aligned(out, size_of(dtype)) || !aligned(pages, 16)) return GSI_ERR_INVALID_ARG;
   for (const int* p : {q_start, kv_len, table})

@@ -62,6 +62,7 @@ struct Cfg {
   static constexpr int kWarpBytes = (kRing + kQ + kSums + kBars + 15) / 16 * 16;
   static constexpr int kSmem = kWarps * kWarpBytes;
   static constexpr int kSnap = kTiles == 1 ? 4 : 2;    // units: the share of a warp ends with a segment that ends as near
+  static constexpr int kCost = L;                      // units that a segment itself counts as in a share
   static constexpr int kPart = kPartFloats(G);
   static constexpr int kPartRows = kPart / (kDim + 8);
 };
@@ -110,10 +111,16 @@ struct Seq {
   __device__ __forceinline__ long long all(const Shape& s) const { return segments(s) * units; }
 };
 // a / b of numbers that are not negative and seldom large
+__device__ __noinline__ long long large_quotient(long long a, long long b) { return a / b; }
 __device__ __forceinline__ long long quotient(long long a, long long b) {
-  if ((a | b) >> 32) return a / b;
+  if ((a | b) >> 32) return large_quotient(a, b);
   return (unsigned)a / (unsigned)b;
 }
+// Where a share begins: its first unit; the sequence, the first unit of that and the segments before it.
+struct Begin {
+  long long u, base, segments;
+  int seq;
+};
 template <int kRows, int kTiles>
 __device__ __forceinline__ Seq load_seq(const Shape& s, const AttendArgs& a, int i) {
   Seq q;
@@ -129,7 +136,9 @@ __device__ __forceinline__ Seq load_seq(const Shape& s, const AttendArgs& a, int
   return q;
 }
 
-// A segment that warps share, whose last warp is of this block.
+constexpr int kFew = 8;   // parts that the last warp of a segment sums by itself
+
+// A segment that more warps share, whose last warp is of this block.
 struct Pending {
   int first, parts, rows;
   long long out[kMaxRows];
@@ -139,9 +148,11 @@ template <int G, int T, int L, int NT>
 __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a, Control* ctl) {
   using C = Cfg<G, T, L, NT>;
   constexpr int kLR = C::kLaneRows, N = C::kTiles;
+  static_assert(C::kRing >= (int)sizeof(Scan2) * kThreads, "prefixes lie in the first warp's rings");
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ Scan2 s_warp[kWarps];
-  __shared__ long long s_before[kThreads];   // units before a thread's sequences
+  Scan2* s_before = reinterpret_cast<Scan2*>(smem);   // units and segments before a thread's sequences (where the rings will be)
+  __shared__ Begin s_begin[kWarps * 2];
   __shared__ Pending s_pending[kWarps * 2];
   __shared__ int s_n_pending;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gr = lane >> 2, t4 = lane & 3;
@@ -168,40 +179,46 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
     sum.a += x.all(s);
     sum.b += x.segments(s);
   }
-  s_before[tid] = block_scan(sum, &total, s_warp).a;
-  const long long shares = max(1ll, min((long long)kMaxShares, max(total.a / C::kSnap, total.b)));
-  const int share = warp * kGrid + blockIdx.x;   // (few shares: one a block)
-  const bool any = total.a > 0 && share < shares;
-  if (total.a == 0 || blockIdx.x >= shares) return;
+  s_before[tid] = block_scan(sum, &total, s_warp);
+  if (total.a == 0) return;
+  // (a segment counts as kCost units more: its rows have to be fetched and its sums to be put away)
+  const long long weight = total.a + C::kCost * total.b;
+  const long long shares = max(1ll, min((long long)kMaxShares, max(quotient(weight, C::kSnap + C::kCost), total.b)));
+  if (blockIdx.x >= shares) return;
   __syncthreads();
-  // where a share begins: the unit, its sequence and that one's first unit
-  auto begin_of = [&](int x_share, int* x_seq, long long* x_base) {
-    const long long x = quotient(total.a * x_share, shares);
-    if (x >= total.a) return total.a;
-    int lo = 0, hi = kThreads;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (s_before[mid] <= x) lo = mid;
-      else hi = mid;
+  if (tid < kWarps * 2) {   // the shares of the block's warps, and those behind them.  (Few shares: one a block.)
+    const long long x = quotient(weight * ((tid >> 1) * kGrid + blockIdx.x + (tid & 1)), shares);
+    Begin at{total.a, 0, 0, 0};
+    if (x < weight) {
+      int lo = 0, hi = kThreads;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s_before[mid].a + C::kCost * s_before[mid].b <= x) lo = mid;
+        else hi = mid;
+      }
+      at = {0, s_before[lo].a, s_before[lo].b, lo * per};
+      Seq q = load(at.seq);
+      for (;;) {
+        const long long n = q.segments(s);
+        if (x < at.base + C::kCost * at.segments + n * (q.units + C::kCost)) break;
+        at.base += n * q.units;
+        at.segments += n;
+        q = load(++at.seq);
+      }
+      const long long in = x - at.base - C::kCost * at.segments, segment = quotient(in, q.units + C::kCost);
+      const int unit = max((int)(in - segment * (q.units + C::kCost)) - C::kCost, 0), left = q.units - unit;
+      at.u = at.base + segment * q.units + (unit < C::kSnap && unit <= left ? 0 : left < C::kSnap ? q.units : unit);
     }
-    long long base = s_before[lo];
-    int i = lo * per;
-    Seq q = load(i);
-    for (long long n; x >= base + (n = q.all(s));) {
-      base += n;
-      q = load(++i);
-    }
-    *x_seq = i;
-    *x_base = base;
-    const long long begin = base + quotient(x - base, q.units) * q.units, from = x - begin, to = begin + q.units - x;
-    return from < C::kSnap && from <= to ? begin : to < C::kSnap ? begin + q.units : x;
-  };
+    s_begin[tid] = at;
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncthreads();
+  const int share = warp * kGrid + blockIdx.x;
 
-  if (any) {
-    int seq = 0;
-    long long base = 0, skip_base;
-    int skip_seq;
-    const long long u0 = begin_of(share, &seq, &base), u1 = begin_of(share + 1, &skip_seq, &skip_base);
+  if (share < shares) {
+    const long long u0 = s_begin[warp * 2].u, u1 = s_begin[warp * 2 + 1].u;
+    long long base = s_begin[warp * 2].base, segment = s_begin[warp * 2].segments;   // the next one, counted over all sequences
+    int seq = s_begin[warp * 2].seq;
     const int mine = (int)(u1 - u0);   // the warp's units
     Seq q;
     int head = 0, row_tile = 0, unit = 0;   // of the next unit
@@ -209,12 +226,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       q = load(seq);
       while (u0 >= base + q.all(s)) {   // (the share begins where the sequence ended)
         base += q.all(s);
+        segment += q.segments(s);
         q = load(++seq);
       }
-      const long long segment = quotient(u0 - base, q.units);
-      unit = (int)(u0 - base - segment * q.units);
-      head = (int)quotient(segment, q.n_row_tiles);
-      row_tile = (int)(segment - (long long)head * q.n_row_tiles);
+      const int first = (int)quotient(u0 - base, q.units);
+      segment += first;
+      unit = (int)(u0 - base - (long long)first * q.units);
+      head = (int)((unsigned)first / (unsigned)q.n_row_tiles);
+      row_tile = first - head * q.n_row_tiles;
     }
 
     // ---- its tiles come through two rings, K and V; lane (N j + i) % 32 knows where tile i of unit j lies
@@ -248,7 +267,6 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
     // K (V) of unit j, if there is one, to its stage
     auto issue = [&](int j, int stage, bool of_v) {
       if (j >= mine) return;
-      if (!of_v && j % (32 / N) == 0) look_up(j / (32 / N));
       if (lane / N == j % (32 / N)) {
         uint64_t* bar = bars + (of_v ? C::kStages : 0) + stage;
         if (where) {
@@ -259,10 +277,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
         }
       }
     };
-    for (int i = 0; i < C::kStages; ++i) {
-      issue(i, i, false);
-      issue(i, i, true);
-    }
+    if (mine > 0) look_up(0);
+#pragma unroll 1
+    for (int i = 0; i < 2 * C::kStages; ++i) issue(i >> 1, i >> 1, i & 1);
     int stage = 0;
     uint32_t phase = 0;
     bool gave_up = false;    // a copy did not arrive
@@ -571,6 +588,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       for (int pos = unit * N * kTile; j < end; pos += N * kTile) {
         if (__any_sync(0xffffffffu, !mbar_wait(bars + stage, phase))) gave_up = true;
         if (gave_up) break;
+        if ((j + C::kStages) % (32 / N) == 0 && j + C::kStages < mine) look_up((j + C::kStages) / (32 / N));
         const unsigned missing = ((j & 32 / N) ? bad_odd : bad_even) >> j % (32 / N) * N & ((1u << N) - 1);   // tiles that have no page
         if (missing && lane == 0) ctl->status = GSI_ERR_INVALID_ARG;
         if (least - pos >= N * kTile && !missing) {
@@ -660,15 +678,50 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
         }
       if (!whole) {
         // the boundaries between shares that lie within the segment: shares first .. first + n_parts - 1 have a part
-        const long long begin = u0 + (end - n_units) - unit, behind = begin + q.units;
-        const long long b1 = quotient((begin + C::kSnap) * shares + total.a - 1, total.a);
-        const long long b2 = quotient((behind - C::kSnap + 1) * shares + total.a - 1, total.a) - 1;
+        const long long begin = u0 + (end - n_units) - unit + C::kCost * (segment + 1);   // with what the segments count as
+        const long long b1 = quotient((begin + C::kSnap) * shares + weight - 1, weight);
+        const long long b2 = quotient((begin + q.units - C::kSnap + 1) * shares + weight - 1, weight) - 1;
         const int first = (int)b1 - 1, n_parts = (int)(b2 - b1) + 2;
         __threadfence();
         __syncwarp();
-        if (lane == 0 && atomicAdd(a.tickets + first, 1u) == (unsigned)n_parts - 1) {
-          a.tickets[first] = 0u;
-          __threadfence();
+        bool last = false;
+        if (lane == 0) {
+          last = atomicAdd(a.tickets + first, 1u) == (unsigned)n_parts - 1;
+          if (last) {
+            a.tickets[first] = 0u;
+            __threadfence();
+          }
+        }
+        last = __any_sync(0xffffffffu, last);
+        if (last && n_parts <= kFew) {
+#pragma unroll 1
+          for (int i = lane; i < n_rows * (C::kDim / 4); i += 32) {
+            const int r = i / (C::kDim / 4), c4 = i % (C::kDim / 4);
+            float2 ml[kFew];
+            float4 px[kFew];
+            float top = kNone;
+#pragma unroll
+            for (int y = 0; y < kFew; ++y) {
+              const float* from = a.parts + (2ll * (first + min(y, n_parts - 1)) + (y == 0)) * C::kPart;
+              ml[y] = __ldcg(reinterpret_cast<const float2*>(from + C::kPartRows * C::kDim) + r);
+              px[y] = __ldcg(reinterpret_cast<const float4*>(from + r * C::kDim) + c4);
+            }
+#pragma unroll
+            for (int y = 0; y < kFew; ++y)
+              if (y < n_parts) top = fmaxf(top, ml[y].x);
+            float all = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int y = 0; y < kFew; ++y) {
+              if (y >= n_parts) continue;
+              const float f = exp2_fast(ml[y].x - top);
+              all += ml[y].y * f;
+              v[0] += px[y].x * f, v[1] += px[y].y * f, v[2] += px[y].z * f, v[3] += px[y].w * f;
+            }
+            const long long to = (long long)(q.q0 + step_row(r)) * a.out_token + q_head(r) * a.out_head + c4 * 4;
+            for (int e = 0; e < 4; ++e)
+              if (c4 * 4 + e < s.head_dim) store_from_float(a.out, a.dtype, to + e, all == 0.f ? 0.f : v[e] / all);
+          }
+        } else if (last && lane == 0) {
           Pending& x = s_pending[atomicAdd(&s_n_pending, 1)];
           x.first = first;
           x.parts = n_parts;
@@ -680,6 +733,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       unit += n_units;
       if (unit == q.units) {
         unit = 0;
+        ++segment;
         if (++row_tile == q.n_row_tiles) {
           row_tile = 0;
           if (++head == s.n_heads) {
@@ -703,7 +757,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
     }
   }
 
-  // ---- segments that several warps share, by the block of the last of them: its threads take four channels each of
+  // ---- segments that many warps share, by the block of the last of them: its threads take four channels each of
   // every kSets-th part
   __syncthreads();
   constexpr int kLanes = C::kDim / 4, kSets = kThreads / kLanes / (kThreads % kLanes ? 2 : 1);
@@ -716,18 +770,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       if (set < kSets) {
         float top = kNone, all = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int y0 = set; y0 < x.parts; y0 += 4 * kSets) {
-          float2 ml[4];
-          float4 px[4];
+        for (int y0 = set; y0 < x.parts; y0 += kFew * kSets) {
+          float2 ml[kFew];
+          float4 px[kFew];
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
+          for (int y = 0; y < kFew; ++y) {
             const int b = min(y0 + y * kSets, x.parts - 1);
             const float* from = a.parts + (2ll * (x.first + b) + (b == 0)) * C::kPart;
             ml[y] = __ldcg(reinterpret_cast<const float2*>(from + C::kPartRows * C::kDim) + r);
             px[y] = __ldcg(reinterpret_cast<const float4*>(from + r * C::kDim) + c4);
           }
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
+          for (int y = 0; y < kFew; ++y) {
             if (y0 + y * kSets >= x.parts) continue;
             const float next = fmaxf(top, ml[y].x), keep = exp2_fast(top - next), f = exp2_fast(ml[y].x - next);
             top = next;
@@ -761,7 +815,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
 template <int G, int T, int L, int NT>
 cudaError_t launch(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
   using C = Cfg<G, T, L, NT>;
-  static_assert(C::kSmem + 5120 <= 115712, "two blocks of an SM, with what else they hold in shared memory");
+  static_assert(C::kSmem + 4096 <= 115712, "two blocks of an SM, with what else they hold in shared memory");
   static_assert(C::kRows <= C::kPartRows && 4 * NT <= C::kPartRows && C::kHalf % 16 == 0 && C::kStages >= 1, "layout");
   if (!a.q) return cudaFuncSetAttribute(k_kv_attend<G, T, L, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   k_kv_attend<G, T, L, NT><<<kGrid, kThreads, C::kSmem, stream>>>(s, a, ctl);
