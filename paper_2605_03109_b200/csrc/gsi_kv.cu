@@ -556,7 +556,7 @@ gsi_status_t gsi_kv_attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t
   if (!h || !is_type(dtype) || n_rows < 0 || n_q_heads <= 0 || n_q_heads % h->shape.n_heads || n_seqs <= 0 || n_seqs > h->shape.max_seqs ||
       !std::isfinite(scale))
     return GSI_ERR_INVALID_ARG;
-  if ((long long)n_rows * n_q_heads >= 1ll << 31) return GSI_ERR_UNSUPPORTED;
+  if ((long long)n_rows * n_q_heads >= 1ll << 31 || n_q_heads / h->shape.n_heads > kv::kMaxShared) return GSI_ERR_UNSUPPORTED;
   if (n_rows == 0) return GSI_OK;
   if (!aligned(q, size_of(dtype)) || !aligned(out, size_of(dtype)) || !aligned(pages, 16)) return GSI_ERR_INVALID_ARG;
   for (const int* p : {q_start, kv_len, table})
@@ -565,7 +565,7 @@ gsi_status_t gsi_kv_attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t
   const gsi_status_t st = on_device(h);
   if (st != GSI_OK) return st;
   const kv::AttendArgs a{q, out, dtype, q_token_stride, q_head_stride, out_token_stride, out_head_stride, n_rows, n_q_heads,
-                         n_q_heads / h->shape.n_heads, (float)(scale * 1.4426950408889634), q_start, kv_len, table, n_seqs, static_cast<const unsigned char*>(pages),
+                         n_q_heads / h->shape.n_heads, 1.f / (n_q_heads / h->shape.n_heads), (float)(scale * 1.4426950408889634), q_start, kv_len, table, n_seqs, static_cast<const unsigned char*>(pages),
                          h->parts, h->tickets};
   return launched(h, stream, kv::launch_attend(h->shape, a, h->ctl, stream));
 }

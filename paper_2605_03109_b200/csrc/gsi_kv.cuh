@@ -12,7 +12,8 @@ constexpr int kTile = 16;          // tokens of a tile
 constexpr int kGroup = 64;         // channels that share a pair (s, mid)
 constexpr int kCodeBytes = 512;    // codes of a block: 16 tokens x 64 channels, 16 bytes a lane of a warp
 constexpr int kBlockBytes = 576;   // ... and 16 pairs
-constexpr int kMaxShares = 296 * 8;   // warps of the attention's grid
+constexpr int kMaxShares = 148 * 16;   // warps of the attention's grid
+constexpr int kMaxShared = 1 << 16;    // (x + 1/2) / shared is right to a row for x < shared + kMaxRows
 constexpr int kMaxRows = 16;          // rows of the attention that a warp takes at a time
 // What a warp leaves of rows that it shares with others, for heads of that many blocks.
 constexpr int kPartFloats(int groups) { return (groups <= 2 ? kMaxRows : kMaxRows / 2) * (groups * kGroup + 8); }
@@ -67,7 +68,8 @@ struct AttendArgs {
   void* out;
   gsi_dtype_t dtype;
   long long q_token, q_head, out_token, out_head;
-  int n_rows, n_q_heads, shared;   // shared: q heads of a head of the cache
+  int n_rows, n_q_heads, shared;   // shared: q heads of a head of the cache (up to kMaxShared)
+  float per_shared;                // 1 / shared
   float scale;   // of scores in powers of two
   const int *q_start, *kv_len, *table;
   int n_seqs;

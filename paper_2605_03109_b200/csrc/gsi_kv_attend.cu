@@ -34,9 +34,10 @@ using umma::mbar_init;
 using umma::mbar_wait;
 using umma::s32;
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 16;
 constexpr int kThreads = kWarps * 32;
-constexpr int kGrid = kMaxShares / kWarps;   // two blocks an SM
+constexpr int kScan = 256;      // threads that look through the sequences
+constexpr int kGrid = kMaxShares / kWarps;   // a block an SM (of two, the one that came first ran ahead by an eighth)
 constexpr int kFlush = 32;      // units between sums in fp32 (T = 2)
 constexpr float kLow = 4096.f;  // units of the second term of q in one of the first
 constexpr float kLazy = 8.f;    // a running maximum is left where it is while 2^score stays below 2^kLazy above it
@@ -145,10 +146,10 @@ struct Pending {
 };
 
 template <int G, int T, int L, int NT>
-__global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a, Control* ctl) {
+__global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a, Control* ctl) {
   using C = Cfg<G, T, L, NT>;
   constexpr int kLR = C::kLaneRows, N = C::kTiles;
-  static_assert(C::kRing >= (int)sizeof(Scan2) * kThreads, "prefixes lie in the first warp's rings");
+  static_assert(C::kRing >= (int)sizeof(Scan2) * kScan, "prefixes lie in the first warp's rings");
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ Scan2 s_warp[kWarps];
   Scan2* s_before = reinterpret_cast<Scan2*>(smem);   // units and segments before a thread's sequences (where the rings will be)
@@ -172,14 +173,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
   if (tid == 0) s_n_pending = 0;
 
   // ---- shares: the units of all sequences in order, in even pieces that end with a segment where one ends near
-  const int per = (a.n_seqs + kThreads - 1) / kThreads;
+  const int per = (a.n_seqs + kScan - 1) / kScan;
   Scan2 sum{0, 0}, total;
-  for (int i = tid * per; i < min(tid * per + per, a.n_seqs); ++i) {
+  for (int i = tid * per; tid < kScan && i < min(tid * per + per, a.n_seqs); ++i) {
     const Seq x = load(i);
     sum.a += x.all(s);
     sum.b += x.segments(s);
   }
-  s_before[tid] = block_scan(sum, &total, s_warp);
+  const Scan2 before = block_scan(sum, &total, s_warp);
+  if (tid < kScan) s_before[tid] = before;
   if (total.a == 0) return;
   // (a segment counts as kCost units more: its rows have to be fetched and its sums to be put away)
   const long long weight = total.a + C::kCost * total.b;
@@ -190,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
     const long long x = quotient(weight * ((tid >> 1) * kGrid + blockIdx.x + (tid & 1)), shares);
     Begin at{total.a, 0, 0, 0};
     if (x < weight) {
-      int lo = 0, hi = kThreads;
+      int lo = 0, hi = kScan;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (s_before[mid].a + C::kCost * s_before[mid].b <= x) lo = mid;
@@ -301,8 +303,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
       const int n_units = min(q.units - unit, mine - j);   // of this segment
       const int row0 = row_tile * C::kRows, n_rows = min(C::kRows, q.m * a.shared - row0);
       // row r of the tile: row of the step, q head; its tokens
-      auto step_row = [&](int r) { return (row0 + r) / a.shared; };
-      auto q_head = [&](int r) { return head * a.shared + (row0 + r) % a.shared; };
+      const int step0 = row0 / a.shared, in0 = row0 - step0 * a.shared;
+      auto step_row = [&](int r) { return step0 + __float2int_rd((in0 + r + 0.5f) * a.per_shared); };
+      auto q_head = [&](int r) { return head * a.shared + row0 + r - step_row(r) * a.shared; };
       auto sees = [&](int r) { return q.seen + step_row(min(r, n_rows - 1)) + 1; };
 
       // the rows as B operand, a lane 2 G channels.  (Columns of rows that are not there hold what they held.)
@@ -815,7 +818,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_kv_attend(Shape s, AttendArgs a
 template <int G, int T, int L, int NT>
 cudaError_t launch(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
   using C = Cfg<G, T, L, NT>;
-  static_assert(C::kSmem + 4096 <= 115712, "two blocks of an SM, with what else they hold in shared memory");
+  static_assert(C::kSmem + 6144 <= 232448, "with what else a block holds in shared memory");
   static_assert(C::kRows <= C::kPartRows && 4 * NT <= C::kPartRows && C::kHalf % 16 == 0 && C::kStages >= 1, "layout");
   if (!a.q) return cudaFuncSetAttribute(k_kv_attend<G, T, L, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   k_kv_attend<G, T, L, NT><<<kGrid, kThreads, C::kSmem, stream>>>(s, a, ctl);
