@@ -168,7 +168,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
 
   if (lane == 0)
     for (int i = 0; i < 2 * C::kStages; ++i) mbar_init(bars + i, N);
-  for (int i = lane; i < (C::kQ + C::kSums) / 4; i += 32) reinterpret_cast<uint32_t*>(s_q)[i] = 0u;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   if (tid == 0) s_n_pending = 0;
 
@@ -180,16 +179,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
     sum.a += x.all(s);
     sum.b += x.segments(s);
   }
+  for (int i = lane; i < (C::kQ + C::kSums) / 16; i += 32) reinterpret_cast<uint4*>(s_q)[i] = make_uint4(0u, 0u, 0u, 0u);
   const Scan2 before = block_scan(sum, &total, s_warp);
   if (tid < kScan) s_before[tid] = before;
   if (total.a == 0) return;
   // (a segment counts as kCost units more: its rows have to be fetched and its sums to be put away)
   const long long weight = total.a + C::kCost * total.b;
   const long long shares = max(1ll, min((long long)kMaxShares, max(quotient(weight, C::kSnap + C::kCost), total.b)));
-  if (blockIdx.x >= shares) return;
+  // Few shares: one a block.  Otherwise a block's are neighbours: long segments are then the work of a few blocks each, and
+  // not all of them wait for the slowest one.
+  const bool full = shares == kMaxShares;
+  const int my_share = full ? blockIdx.x * kWarps : blockIdx.x, stride = full ? 1 : kGrid;
+  if (my_share >= shares) return;
   __syncthreads();
-  if (tid < kWarps * 2) {   // the shares of the block's warps, and those behind them.  (Few shares: one a block.)
-    const long long x = quotient(weight * ((tid >> 1) * kGrid + blockIdx.x + (tid & 1)), shares);
+  if (tid < kWarps * 2) {   // the shares of the block's warps, and those behind them
+    const long long x = quotient(weight * (my_share + (tid >> 1) * stride + (tid & 1)), shares);
     Begin at{total.a, 0, 0, 0};
     if (x < weight) {
       int lo = 0, hi = kScan;
@@ -215,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncthreads();
-  const int share = warp * kGrid + blockIdx.x;
+  const int share = my_share + warp * stride;
 
   if (share < shares) {
     const long long u0 = s_begin[warp * 2].u, u1 = s_begin[warp * 2 + 1].u;
@@ -236,6 +240,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
       unit = (int)(u0 - base - (long long)first * q.units);
       head = (int)((unsigned)first / (unsigned)q.n_row_tiles);
       row_tile = first - head * q.n_row_tiles;
+    }
+
+    // The first row of q is asked for ahead of the tiles, which would hold it up; rows of later segments are prefetched.
+    float q_first[2 * G];
+    auto fetch = [&](long long from, float (&v)[2 * G]) {
+#pragma unroll
+      for (int i = 0; i < 2 * G; ++i) {
+        const int c = i * 32 + lane;
+        v[i] = c < s.head_dim ? load_as_float(a.q, a.dtype, from + c) : 0.f;
+      }
+    };
+    // row r of a tile of rows, from the step's row `step0` and the q head `in0` of those that share the head on
+    auto step_of = [&](int in0, int r) { return __float2int_rd((in0 + r + 0.5f) * a.per_shared); };
+    auto q_from = [&](const Seq& x, int of_head, int step0, int in0, int r) {
+      const int i = step_of(in0, r);
+      return (long long)(x.q0 + step0 + i) * a.q_token + (long long)(of_head * a.shared + in0 + r - i * a.shared) * a.q_head;
+    };
+    if (mine > 0) {
+      const int row0 = row_tile * C::kRows, step0 = row0 / a.shared;
+      fetch(q_from(q, head, step0, row0 - step0 * a.shared, 0), q_first);
     }
 
     // ---- its tiles come through two rings, K and V; lane (N j + i) % 32 knows where tile i of unit j lies
@@ -304,20 +328,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
       const int row0 = row_tile * C::kRows, n_rows = min(C::kRows, q.m * a.shared - row0);
       // row r of the tile: row of the step, q head; its tokens
       const int step0 = row0 / a.shared, in0 = row0 - step0 * a.shared;
-      auto step_row = [&](int r) { return step0 + __float2int_rd((in0 + r + 0.5f) * a.per_shared); };
+      auto step_row = [&](int r) { return step0 + step_of(in0, r); };
       auto q_head = [&](int r) { return head * a.shared + row0 + r - step_row(r) * a.shared; };
       auto sees = [&](int r) { return q.seen + step_row(min(r, n_rows - 1)) + 1; };
 
       // the rows as B operand, a lane 2 G channels.  (Columns of rows that are not there hold what they held.)
       for (int r = 0; r < n_rows; ++r) {
         float v[2 * G], top = 0.f;
-        const long long from = (long long)(q.q0 + step_row(r)) * a.q_token + q_head(r) * a.q_head;
+        if (j || r) {
+          fetch(q_from(q, head, step0, in0, r), v);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 2 * G; ++i) {
-          const int c = i * 32 + lane;
-          v[i] = c < s.head_dim ? load_as_float(a.q, a.dtype, from + c) : 0.f;
-          top = fmaxf(top, fabsf(v[i]));
+          for (int i = 0; i < 2 * G; ++i) v[i] = q_first[i];
         }
+#pragma unroll
+        for (int i = 0; i < 2 * G; ++i) top = fmaxf(top, fabsf(v[i]));
 #pragma unroll
         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         // 2^k takes the largest to below 2^11 (2^14), as a product of two; a row of zeros, or with an infinity, stays as it is
@@ -354,6 +379,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
         if (lane == 0) s_factor[r] = fminf(fmaxf(a.scale / k0 * (0x1p24f / k1), -0x1p100f), 0x1p100f);
       }
       __syncwarp();
+      if (j + n_units < mine) {   // the rows of the segment behind
+        Seq x = q;
+        int x_seq = seq, x_head = head, x_tile = row_tile + 1;
+        if (x_tile == x.n_row_tiles) {
+          x_tile = 0;
+          if (++x_head == s.n_heads) {
+            x_head = 0;
+            do x = load(++x_seq);
+            while (x.n_row_tiles == 0);
+          }
+        }
+        const int first = x_tile * C::kRows, n = min(C::kRows, x.m * a.shared - first), x_step = first / a.shared;
+        constexpr int kLines = G * 2 / T;   // of 128 bytes, a row
+        for (int i = lane; i < n * kLines; i += 32) {
+          const char* at = static_cast<const char*>(a.q) +
+                           q_from(x, x_head, x_step, first - x_step * a.shared, i / kLines) * (T == 2 ? 4 : 2) + i % kLines * 128;
+          if (i % kLines * (T == 2 ? 32 : 64) < s.head_dim) asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+        }
+      }
 
       // sums and maxima, of each tile of a unit its own until the segment ends
       float O[NT][G][4][4], z[NT][kLR][G], m[NT][kLR], l[NT][kLR], m_flush[NT], factor[NT][kLR];
@@ -763,52 +807,47 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
   // ---- segments that many warps share, by the block of the last of them: its threads take four channels each of
   // every kSets-th part
   __syncthreads();
-  constexpr int kLanes = C::kDim / 4, kSets = kThreads / kLanes / (kThreads % kLanes ? 2 : 1);
-  float4* s_v = reinterpret_cast<float4*>(smem);                      // [kSets][kLanes]
-  float2* s_ml = reinterpret_cast<float2*>(smem + kSets * kLanes * 16);   // [kSets]
+  constexpr int kLanes = C::kDim / 4, kSets = kThreads / kLanes >= 16 ? 16 : kThreads / kLanes >= 8 ? 8 : 4;
+  static_assert(kMaxShares * 8 + kSets * kLanes * 16 <= C::kSmem, "the rings' memory is free by now");
+  float2* s_ml = reinterpret_cast<float2*>(smem);                          // [parts]: maximum and sum
+  float4* s_v = reinterpret_cast<float4*>(smem + kMaxShares * 8);          // [kSets][kLanes]
+  __shared__ float s_red[kWarps];
   const int n_pending = s_n_pending, set = tid / kLanes, c4 = tid - set * kLanes;
   for (int i = 0; i < n_pending; ++i) {
     const Pending& x = s_pending[i];
+    auto part_of = [&](int y) { return a.parts + (2ll * (x.first + y) + (y == 0)) * C::kPart; };
     for (int r = 0; r < x.rows; ++r) {
+      float top = kNone;
+      for (int y = tid; y < x.parts; y += kThreads) {
+        s_ml[y] = __ldcg(reinterpret_cast<const float2*>(part_of(y) + C::kPartRows * C::kDim) + r);
+        top = fmaxf(top, s_ml[y].x);
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      if (lane == 0) s_red[warp] = top;
+      __syncthreads();
+#pragma unroll
+      for (int y = 0; y < kWarps; ++y) top = fmaxf(top, s_red[y]);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (set < kSets) {
-        float top = kNone, all = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int y0 = set; y0 < x.parts; y0 += kFew * kSets) {
-          float2 ml[kFew];
-          float4 px[kFew];
-#pragma unroll
-          for (int y = 0; y < kFew; ++y) {
-            const int b = min(y0 + y * kSets, x.parts - 1);
-            const float* from = a.parts + (2ll * (x.first + b) + (b == 0)) * C::kPart;
-            ml[y] = __ldcg(reinterpret_cast<const float2*>(from + C::kPartRows * C::kDim) + r);
-            px[y] = __ldcg(reinterpret_cast<const float4*>(from + r * C::kDim) + c4);
-          }
-#pragma unroll
-          for (int y = 0; y < kFew; ++y) {
-            if (y0 + y * kSets >= x.parts) continue;
-            const float next = fmaxf(top, ml[y].x), keep = exp2_fast(top - next), f = exp2_fast(ml[y].x - next);
-            top = next;
-            all = all * keep + ml[y].y * f;
-            v.x = v.x * keep + px[y].x * f, v.y = v.y * keep + px[y].y * f;
-            v.z = v.z * keep + px[y].z * f, v.w = v.w * keep + px[y].w * f;
-          }
+#pragma unroll 8
+        for (int y = set; y < x.parts; y += kSets) {
+          const float4 w = __ldcg(reinterpret_cast<const float4*>(part_of(y) + r * C::kDim) + c4);
+          const float f = exp2_fast(s_ml[y].x - top);
+          v.x += w.x * f, v.y += w.y * f, v.z += w.z * f, v.w += w.w * f;
         }
         s_v[set * kLanes + c4] = v;
-        if (c4 == 0) s_ml[set] = make_float2(top, all);
       }
       __syncthreads();
       if (set == 0) {
-        float top = kNone, all = 0.f;
-        for (int y = 0; y < kSets; ++y) top = fmaxf(top, s_ml[y].x);
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        float all = 0.f, sums[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int y = 0; y < x.parts; ++y) all += s_ml[y].y * exp2_fast(s_ml[y].x - top);
         for (int y = 0; y < kSets; ++y) {
-          const float f = exp2_fast(s_ml[y].x - top);
           const float4 w = s_v[y * kLanes + c4];
-          all += s_ml[y].y * f;
-          v[0] += w.x * f, v[1] += w.y * f, v[2] += w.z * f, v[3] += w.w * f;
+          sums[0] += w.x, sums[1] += w.y, sums[2] += w.z, sums[3] += w.w;
         }
         for (int e = 0; e < 4; ++e)
-          if (c4 * 4 + e < s.head_dim) store_from_float(a.out, a.dtype, x.out[r] + c4 * 4 + e, all == 0.f ? 0.f : v[e] / all);
+          if (c4 * 4 + e < s.head_dim) store_from_float(a.out, a.dtype, x.out[r] + c4 * 4 + e, all == 0.f ? 0.f : sums[e] / all);
       }
       __syncthreads();
     }
