@@ -28,8 +28,6 @@ namespace kv {
 
 namespace {
 
-using umma::mbar_arrive;
-using umma::mbar_expect_tx;
 using umma::mbar_init;
 using umma::mbar_wait;
 using umma::s32;
@@ -63,7 +61,7 @@ struct Cfg {
   static constexpr int kWarpBytes = (kRing + kQ + kSums + kBars + 15) / 16 * 16;
   static constexpr int kSmem = kWarps * kWarpBytes;
   static constexpr int kSnap = kTiles == 1 ? 4 : 2;    // units: the share of a warp ends with a segment that ends as near
-  static constexpr int kCost = L;                      // units that a segment itself counts as in a share
+  static constexpr int kCost = L + 1;                    // units that a segment itself counts as in a share
   static constexpr int kPart = kPartFloats(G);
   static constexpr int kPartRows = kPart / (kDim + 8);
 };
@@ -83,6 +81,25 @@ __device__ __forceinline__ float exp2_fast(float v) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+  return v;
+}
+__device__ __forceinline__ float2 lds_float2(uint32_t at) {
+  const uint2 v = lds64(at);
+  return make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
+}
+__device__ __forceinline__ float lds_float(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
+  return v;
+}
 __device__ __forceinline__ float2 unpack_half2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
@@ -98,9 +115,9 @@ __device__ __forceinline__ uint32_t centred(uint32_t w) {
   else h = __hadd2(h, __half2half2(__ushort_as_half(0xE408)));   // - 1032
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ void copy_tile(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+__device__ __forceinline__ void copy_half(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
-               "r"(s32(bar))
+               "r"(bar)
                : "memory");
 }
 
@@ -243,13 +260,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
     }
 
     // The first row of q is asked for ahead of the tiles, which would hold it up; rows of later segments are prefetched.
-    float q_first[2 * G];
-    auto fetch = [&](long long from, float (&v)[2 * G]) {
+    uint32_t q_first[2 * G];   // as it lies there
+    auto fetch = [&](long long from, uint32_t (&v)[2 * G]) {
 #pragma unroll
       for (int i = 0; i < 2 * G; ++i) {
         const int c = i * 32 + lane;
-        v[i] = c < s.head_dim ? load_as_float(a.q, a.dtype, from + c) : 0.f;
+        v[i] = 0u;
+        if (c < s.head_dim) v[i] = T == 2 ? __ldg(static_cast<const uint32_t*>(a.q) + from + c) : __ldg(static_cast<const uint16_t*>(a.q) + from + c);
       }
+    };
+    auto as_float = [&](uint32_t v) {
+      return T == 2 ? __uint_as_float(v) : a.dtype == GSI_BF16 ? __uint_as_float(v << 16) : __half2float(__ushort_as_half((unsigned short)v));
     };
     // row r of a tile of rows, from the step's row `step0` and the q head `in0` of those that share the head on
     auto step_of = [&](int in0, int r) { return __float2int_rd((in0 + r + 0.5f) * a.per_shared); };
@@ -290,37 +311,41 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
       if (batch & 1) bad_odd = mask;
       else bad_even = mask;
     };
-    // K (V) of unit j, if there is one, to its stage
-    auto issue = [&](int j, int stage, bool of_v) {
-      if (j >= mine) return;
-      if (lane / N == j % (32 / N)) {
-        uint64_t* bar = bars + (of_v ? C::kStages : 0) + stage;
-        if (where) {
-          mbar_expect_tx(bar, C::kHalf);
-          copy_tile(s32(of_v ? ring_v : ring_k) + (stage * N + lane % N) * C::kHalf, where + (of_v ? C::kHalf : 0), C::kHalf, bar);
-        } else {
-          mbar_arrive(bar);
-        }
-      }
-    };
-    if (mine > 0) look_up(0);
-#pragma unroll 1
-    for (int i = 0; i < 2 * C::kStages; ++i) issue(i >> 1, i >> 1, i & 1);
     int stage = 0;
     uint32_t phase = 0;
     bool gave_up = false;    // a copy did not arrive
 
     // what of the columns' operands is of tile i: the columns of the others are zero
     uint32_t only[N];
-    const unsigned char* q_at[N];
+    uint32_t q_at[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const bool of = gr / (2 * L) == i;
       only[i] = of ? ~0u : 0u;
-      q_at[i] = s_q + ((N == 1 || of ? gr % (2 * L) : 2 * L) * 4 + t4) * 16;
+      q_at[i] = s32(s_q) + ((N == 1 || of ? gr % (2 * L) : 2 * L) * 4 + t4) * 16;
     }
     const int my_tile = t4 / L;   // the one whose scores this lane has
+    const uint32_t k_ring = s32(ring_k), v_ring = s32(ring_v), start_at = s32(s_start), sum_at = s32(s_sum);
+    const uint32_t my_pair = my_tile * C::kHalf + kCodeBytes + gr * 8, my_codes = lane * 16;
+    const uint32_t my_k = k_ring + lane % N * C::kHalf, my_v = v_ring + lane % N * C::kHalf;   // where its copies go, and their barriers
+    const uint32_t my_bar = s32(bars);
     auto row_of = [&](int n, int r) { return T == 2 ? n * L + t4 % L : n * 2 * L + t4 % L * 2 + r; };
+
+    // K (V) of unit j, if there is one, to its stage
+    auto issue = [&](int j, int stage, bool of_v) {
+      if (j < mine && lane / N == j % (32 / N)) {
+        const uint32_t bar = my_bar + ((of_v ? C::kStages : 0) + stage) * 8;
+        if (where) {
+          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(C::kHalf) : "memory");
+          copy_half((of_v ? my_v : my_k) + stage * N * C::kHalf, where + (of_v ? C::kHalf : 0), C::kHalf, bar);
+        } else {
+          asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+        }
+      }
+    };
+    if (mine > 0) look_up(0);
+#pragma unroll 1
+    for (int i = 0; i < 2 * C::kStages; ++i) issue(i >> 1, i >> 1, i & 1);
 
     // ---- segments of the share
     for (int j = 0; j < mine && !gave_up;) {
@@ -334,15 +359,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
 
       // the rows as B operand, a lane 2 G channels.  (Columns of rows that are not there hold what they held.)
       for (int r = 0; r < n_rows; ++r) {
+        if (j || r) fetch(q_from(q, head, step0, in0, r), q_first);
         float v[2 * G], top = 0.f;
-        if (j || r) {
-          fetch(q_from(q, head, step0, in0, r), v);
-        } else {
 #pragma unroll
-          for (int i = 0; i < 2 * G; ++i) v[i] = q_first[i];
+        for (int i = 0; i < 2 * G; ++i) {
+          v[i] = as_float(q_first[i]);
+          top = fmaxf(top, fabsf(v[i]));
         }
-#pragma unroll
-        for (int i = 0; i < 2 * G; ++i) top = fmaxf(top, fabsf(v[i]));
 #pragma unroll
         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         // 2^k takes the largest to below 2^11 (2^14), as a product of two; a row of zeros, or with an infinity, stays as it is
@@ -429,35 +452,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
         const int pos = first_pos + my_tile * kTile + gr;
         const bool wrong = kMasked && (missing >> my_tile & 1u);
         float S[NT][kLR][2], p[NT][kLR][2];
-        const unsigned char* k_at = ring_k + stage * N * C::kHalf;
-        const unsigned char* v_at = ring_v + stage * N * C::kHalf;
+        const uint32_t k_at = k_ring + stage * N * C::kHalf, v_at = v_ring + stage * N * C::kHalf;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          const uint2 pw = reinterpret_cast<const uint2*>(k_at + my_tile * C::kHalf + g * kBlockBytes + kCodeBytes)[gr];
+          const uint2 pw = lds64(k_at + my_pair + g * kBlockBytes);
           float acc[NT][4];
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             // -8 times the sum of the column's q: the sums are those of code - 8
             if constexpr (T == 2) {
-              const float2 v = reinterpret_cast<const float2*>(s_start)[g * C::kRows + row_of(n, 0)];
+              const float2 v = lds_float2(start_at + (g * C::kRows + row_of(n, 0)) * 8);
               acc[n][0] = acc[n][2] = v.x;
               acc[n][1] = acc[n][3] = v.y;
             } else {
-              const float4 v = reinterpret_cast<const float4*>(s_start)[(g * C::kRows + row_of(n, 0)) / 2];
-              acc[n][0] = acc[n][2] = v.x;
-              acc[n][1] = acc[n][3] = v.z;
+              acc[n][0] = acc[n][2] = lds_float(start_at + (g * C::kRows + row_of(n, 0)) * 8);
+              acc[n][1] = acc[n][3] = lds_float(start_at + (g * C::kRows + row_of(n, 1)) * 8);
             }
           }
 #pragma unroll
           for (int i = 0; i < N; ++i) {
-            const uint4 w = reinterpret_cast<const uint4*>(k_at + i * C::kHalf + g * kBlockBytes)[lane];
+            const uint4 w = lds128(k_at + my_codes + (i * C::kHalf + g * kBlockBytes));
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const uint32_t x = h ? w.y : w.x, y = h ? w.w : w.z;
               const uint32_t x8 = x >> 8, y8 = y >> 8;
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
-                const uint4 bq = *reinterpret_cast<const uint4*>(q_at[i] + ((n * G + g) * 2 + h) * 512);
+                const uint4 bq = lds128(q_at[i] + ((n * G + g) * 2 + h) * 512);
                 mma_f16(acc[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, bq.x, bq.y);
                 mma_f16(acc[n], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, bq.z, bq.w);
               }
@@ -468,7 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < kLR; ++r) {
-              const float qs = s_sum[g * C::kRows + row_of(n, r)];
+              const float qs = lds_float(sum_at + (g * C::kRows + row_of(n, r)) * 4);
               const float a0 = T == 2 ? fmaf(acc[n][1], 1.f / kLow, acc[n][0]) : acc[n][r];
               const float a1 = T == 2 ? fmaf(acc[n][3], 1.f / kLow, acc[n][2]) : acc[n][2 + r];
               S[n][r][0] = fmaf(p0.x, a0, g ? fmaf(p0.y, qs, S[n][r][0]) : p0.y * qs);
@@ -486,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
         __half2 steps = __half2half2(__ushort_as_half(0));
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          pv[g] = reinterpret_cast<const uint2*>(v_at + my_tile * C::kHalf + g * kBlockBytes + kCodeBytes)[gr];
+          pv[g] = lds64(v_at + my_pair + g * kBlockBytes);
           if constexpr (kMasked) {   // (behind the last token lies anything)
             if (wrong || pos >= q.len) pv[g].x = 0u;
             if (wrong || pos + 8 >= q.len) pv[g].y = 0u;
@@ -590,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
           }
 #pragma unroll
           for (int i = 0; i < N; ++i) {
-            const uint4 w = reinterpret_cast<const uint4*>(v_at + i * C::kHalf + g * kBlockBytes)[lane];
+            const uint4 w = lds128(v_at + my_codes + (i * C::kHalf + g * kBlockBytes));
             const uint32_t x8 = w.x >> 8, y8 = w.y >> 8, z8 = w.z >> 8, w8 = w.w >> 8;
             const uint32_t A[4][4] = {{centred<false>(w.x), centred<false>(w.y), centred<false>(w.z), centred<false>(w.w)},
                                       {centred<true>(w.x), centred<true>(w.y), centred<true>(w.z), centred<true>(w.w)},
