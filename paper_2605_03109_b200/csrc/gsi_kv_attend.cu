@@ -115,10 +115,22 @@ __device__ __forceinline__ uint32_t centred(uint32_t w) {
   else h = __hadd2(h, __half2half2(__ushort_as_half(0xE408)));   // - 1032
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ void copy_half(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
-               "r"(bar)
+__device__ __forceinline__ void copy_half(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint64_t policy) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar), "l"(policy)
                : "memory");
+}
+// Tiles that are read once leave the L2 first: what the next call or the next segment needs (this code, tables, q, parts) would
+// otherwise come from memory, behind the tiles in flight.
+__device__ __forceinline__ uint64_t first_out() {
+  uint64_t policy;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  return policy;
+}
+__device__ __forceinline__ uint64_t as_usual() {
+  uint64_t policy;
+  asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
+  return policy;
 }
 
 // What a step has of one sequence.  Its units: (head, tile of rows, tokens), the last the fastest; those of one head and
@@ -329,6 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
     const uint32_t my_pair = my_tile * C::kHalf + kCodeBytes + gr * 8, my_codes = lane * 16;
     const uint32_t my_k = k_ring + lane % N * C::kHalf, my_v = v_ring + lane % N * C::kHalf;   // where its copies go, and their barriers
     const uint32_t my_bar = s32(bars);
+    const uint64_t policy = L == 4 ? as_usual() : first_out();   // (many rows: other units read the same tiles)
     auto row_of = [&](int n, int r) { return T == 2 ? n * L + t4 % L : n * 2 * L + t4 % L * 2 + r; };
 
     // K (V) of unit j, if there is one, to its stage
@@ -337,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
         const uint32_t bar = my_bar + ((of_v ? C::kStages : 0) + stage) * 8;
         if (where) {
           asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(C::kHalf) : "memory");
-          copy_half((of_v ? my_v : my_k) + stage * N * C::kHalf, where + (of_v ? C::kHalf : 0), C::kHalf, bar);
+          copy_half((of_v ? my_v : my_k) + stage * N * C::kHalf, where + (of_v ? C::kHalf : 0), C::kHalf, bar, policy);
         } else {
           asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
         }
@@ -372,16 +385,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
         int k = (T == 2 ? 137 : 140) - (int)(__float_as_uint(top) >> 23);
         if (top == 0.f || top > 3.402823466e38f) k = 0;
         const float k0 = __uint_as_float((uint32_t)(127 + k / 2) << 23), k1 = __uint_as_float((uint32_t)(127 + k - k / 2) << 23);
-        float part[G], first[G];   // sums of q 2^k (T = 2: of its second term) and of its first term
-#pragma unroll
-        for (int g = 0; g < G; ++g) part[g] = first[g] = 0.f;
 #pragma unroll
         for (int i = 0; i < 2 * G; ++i) {
           const int c = (i & 1) * 32 + lane, g = i >> 1, nib = c & 7;   // channel of the block, of its word
           const float x = v[i] * k0 * k1;
           const float odd = (nib & 1) ? 0.0625f : 1.f, hi = T == 2 ? rintf(x) : x, lo = T == 2 ? rintf((x - hi) * kLow) : 0.f;
-          part[g] += T == 2 ? lo : x;
-          first[g] += hi;
           // word (c % 16) / 8 of lane c / 16: its two steps' registers (nib / 2) % 2, b0 or b1 nib % 2, half nib / 4
           const int col = T == 2 ? r % L * 2 : r % (2 * L), nt = T == 2 ? r / L : r / (2 * L);
           __half* to = reinterpret_cast<__half*>(s_q + ((nt * G + g) * 2 + (c % 16) / 8) * 512 + (col * 4 + c / 16) * 16) + (nib / 2 % 2) * 4 +
@@ -389,18 +397,37 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
           *to = __float2half_rn(hi * odd);
           if constexpr (T == 2) to[32] = __float2half_rn(lo * odd);   // the next column: 4 lanes of 16 bytes on
         }
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          part[g] = warp_sum(part[g]);
-          if constexpr (T == 2) first[g] = warp_sum(first[g]);
-          if (lane == 0) {   // (all in units of the scores' sums: codes enter as code 2^-24)
-            s_sum[g * C::kRows + r] = (T == 2 ? fmaf(part[g], 1.f / kLow, first[g]) : part[g]) * 0x1p-24f;
-            s_start[(g * C::kRows + r) * 2] = (T == 2 ? first[g] : part[g]) * (-8.f * 0x1p-24f);
-            s_start[(g * C::kRows + r) * 2 + 1] = part[g] * (-8.f * 0x1p-24f);
-          }
-        }
         if (lane == 0) s_factor[r] = fminf(fmaxf(a.scale / k0 * (0x1p24f / k1), -0x1p100f), 0x1p100f);
       }
+      __syncwarp();
+      // Per block, what the scores' sums begin with, -8 times the sum of the column's q (the sums are then those of
+      // code - 8), as the sums for codes that are all -8; and the sum of the row's q.
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint4 bq = lds128(s32(s_q) + ((n * G + g) * 2 + h) * 512 + (gr % (2 * L) * 4 + t4) * 16);
+            mma_f16(acc, 0x80088008u, 0x80088008u, 0x80808080u, 0x80808080u, bq.x, bq.y);
+            mma_f16(acc, 0x80088008u, 0x80088008u, 0x80808080u, 0x80808080u, bq.z, bq.w);
+          }
+          if (gr == 0 && t4 < L) {
+            if constexpr (T == 2) {
+              const int r = g * C::kRows + row_of(n, 0);
+              s_start[2 * r] = acc[0];
+              s_start[2 * r + 1] = acc[1];
+              s_sum[r] = fmaf(acc[1], 1.f / kLow, acc[0]) * -0.125f;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                s_start[2 * (g * C::kRows + row_of(n, e))] = acc[e];
+                s_sum[g * C::kRows + row_of(n, e)] = acc[e] * -0.125f;
+              }
+            }
+          }
+        }
       __syncwarp();
       if (j + n_units < mine) {   // the rows of the segment behind
         Seq x = q;
@@ -830,7 +857,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
   __syncthreads();
   constexpr int kLanes = C::kDim / 4, kSets = kThreads / kLanes >= 16 ? 16 : kThreads / kLanes >= 8 ? 8 : 4;
   static_assert(kMaxShares * 8 + kSets * kLanes * 16 <= C::kSmem, "the rings' memory is free by now");
-  float2* s_ml = reinterpret_cast<float2*>(smem);                          // [parts]: maximum and sum
+  float2* s_ml = reinterpret_cast<float2*>(smem);                          // [parts]: maximum and sum, then the weight
   float4* s_v = reinterpret_cast<float4*>(smem + kMaxShares * 8);          // [kSets][kLanes]
   __shared__ float s_red[kWarps];
   const int n_pending = s_n_pending, set = tid / kLanes, c4 = tid - set * kLanes;
@@ -838,7 +865,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
     const Pending& x = s_pending[i];
     auto part_of = [&](int y) { return a.parts + (2ll * (x.first + y) + (y == 0)) * C::kPart; };
     for (int r = 0; r < x.rows; ++r) {
-      float top = kNone;
+      float top = kNone, all = 0.f;
       for (int y = tid; y < x.parts; y += kThreads) {
         s_ml[y] = __ldcg(reinterpret_cast<const float2*>(part_of(y) + C::kPartRows * C::kDim) + r);
         top = fmaxf(top, s_ml[y].x);
@@ -849,20 +876,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
       __syncthreads();
 #pragma unroll
       for (int y = 0; y < kWarps; ++y) top = fmaxf(top, s_red[y]);
+      for (int y = tid; y < x.parts; y += kThreads) {
+        const float f = exp2_fast(s_ml[y].x - top);
+        all += s_ml[y].y * f;
+        s_ml[y].x = f;
+      }
+      all = warp_sum(all);
+      __syncthreads();
+      if (lane == 0) s_red[warp] = all;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (set < kSets) {
 #pragma unroll 8
         for (int y = set; y < x.parts; y += kSets) {
           const float4 w = __ldcg(reinterpret_cast<const float4*>(part_of(y) + r * C::kDim) + c4);
-          const float f = exp2_fast(s_ml[y].x - top);
+          const float f = s_ml[y].x;
           v.x += w.x * f, v.y += w.y * f, v.z += w.z * f, v.w += w.w * f;
         }
         s_v[set * kLanes + c4] = v;
       }
       __syncthreads();
       if (set == 0) {
-        float all = 0.f, sums[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int y = 0; y < x.parts; ++y) all += s_ml[y].y * exp2_fast(s_ml[y].x - top);
+        float sums[4] = {0.f, 0.f, 0.f, 0.f};
+        all = 0.f;
+#pragma unroll
+        for (int y = 0; y < kWarps; ++y) all += s_red[y];
         for (int y = 0; y < kSets; ++y) {
           const float4 w = s_v[y * kLanes + c4];
           sums[0] += w.x, sums[1] += w.y, sums[2] += w.z, sums[3] += w.w;
