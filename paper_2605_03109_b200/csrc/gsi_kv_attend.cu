@@ -32,10 +32,8 @@ using umma::mbar_init;
 using umma::mbar_wait;
 using umma::s32;
 
-constexpr int kWarps = 16;
-constexpr int kThreads = kWarps * 32;
 constexpr int kScan = 256;      // threads that look through the sequences
-constexpr int kGrid = kMaxShares / kWarps;   // a block an SM (of two, the one that came first ran ahead by an eighth)
+constexpr int kGrid = 148;      // a block an SM (of two, the one that came first ran ahead by an eighth)
 constexpr int kFlush = 32;      // units between sums in fp32 (T = 2)
 constexpr float kLow = 4096.f;  // units of the second term of q in one of the first
 constexpr float kLazy = 8.f;    // a running maximum is left where it is while 2^score stays below 2^kLazy above it
@@ -48,18 +46,23 @@ constexpr float kNone = -3e38f; // the maximum of no score
 // Few rows so share the scalar work of a tile's scores, where they would leave most columns empty.
 template <int G, int T, int L, int NT>
 struct Cfg {
+  // Twelve warps where sixteen would leave too few registers: what is spilled comes back behind the tiles in flight.
+  static constexpr int kWarps = G >= 3 || G * NT == 4 ? 12 : 16;
+  static constexpr int kThreads = kWarps * 32;
+  static constexpr int kShares = kGrid * kWarps;
   static constexpr int kDim = G * kGroup;
   static constexpr int kTiles = 4 / L;                 // of a unit
   static constexpr int kLaneRows = T == 1 ? 2 : 1;     // rows of a lane per column tile
   static constexpr int kRows = NT * L * kLaneRows;     // rows of a unit
   static constexpr int kHalf = G * kBlockBytes;        // K of a tile, or V
-  static constexpr int kStages = (G == 1 ? 8 : G == 2 ? 4 : 2) / kTiles;   // units under way
+  static constexpr int kStages = (kWarps == 16 ? 9216 : 14336) / (2 * kHalf) / kTiles;   // units under way
   static constexpr int kRing = kStages * kTiles * 2 * kHalf;
   static constexpr int kQ = NT * G * 1024;
   static constexpr int kSums = ((3 * G + 1) * kRows * 4 + 15) / 16 * 16;   // per block: -8 times the sums of q's terms, the sum of q; factors
   static constexpr int kBars = kStages * 2 * 8;
   static constexpr int kWarpBytes = (kRing + kQ + kSums + kBars + 15) / 16 * 16;
   static constexpr int kSmem = kWarps * kWarpBytes;
+  static_assert(kShares <= kMaxShares, "the workspace's parts and tickets");
   static constexpr int kSnap = kTiles == 1 ? 4 : 2;    // units: the share of a warp ends with a segment that ends as near
   static constexpr int kCost = L + 1;                    // units that a segment itself counts as in a share
   static constexpr int kPart = kPartFloats(G);
@@ -175,9 +178,9 @@ struct Pending {
 };
 
 template <int G, int T, int L, int NT>
-__global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a, Control* ctl) {
+__global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Shape s, AttendArgs a, Control* ctl) {
   using C = Cfg<G, T, L, NT>;
-  constexpr int kLR = C::kLaneRows, N = C::kTiles;
+  constexpr int kLR = C::kLaneRows, N = C::kTiles, kWarps = C::kWarps, kThreads = C::kThreads;
   static_assert(C::kRing >= (int)sizeof(Scan2) * kScan, "prefixes lie in the first warp's rings");
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ Scan2 s_warp[kWarps];
@@ -214,10 +217,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
   if (total.a == 0) return;
   // (a segment counts as kCost units more: its rows have to be fetched and its sums to be put away)
   const long long weight = total.a + C::kCost * total.b;
-  const long long shares = max(1ll, min((long long)kMaxShares, max(quotient(weight, C::kSnap + C::kCost), total.b)));
+  const long long shares = max(1ll, min((long long)C::kShares, max(quotient(weight, C::kSnap + C::kCost), total.b)));
   // Few shares: one a block.  Otherwise a block's are neighbours: long segments are then the work of a few blocks each, and
   // not all of them wait for the slowest one.
-  const bool full = shares == kMaxShares;
+  const bool full = shares == C::kShares;
   const int my_share = full ? blockIdx.x * kWarps : blockIdx.x, stride = full ? 1 : kGrid;
   if (my_share >= shares) return;
   __syncthreads();
@@ -372,13 +375,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
 
       // the rows as B operand, a lane 2 G channels.  (Columns of rows that are not there hold what they held.)
       for (int r = 0; r < n_rows; ++r) {
-        if (j || r) fetch(q_from(q, head, step0, in0, r), q_first);
+        if (j && r == 0) fetch(q_from(q, head, step0, in0, 0), q_first);
         float v[2 * G], top = 0.f;
 #pragma unroll
         for (int i = 0; i < 2 * G; ++i) {
           v[i] = as_float(q_first[i]);
           top = fmaxf(top, fabsf(v[i]));
         }
+        if (r + 1 < n_rows) fetch(q_from(q, head, step0, in0, r + 1), q_first);
 #pragma unroll
         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         // 2^k takes the largest to below 2^11 (2^14), as a product of two; a row of zeros, or with an infinity, stays as it is
@@ -855,7 +859,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attend(Shape s, AttendArgs a
   // ---- segments that many warps share, by the block of the last of them: its threads take four channels each of
   // every kSets-th part
   __syncthreads();
-  constexpr int kLanes = C::kDim / 4, kSets = kThreads / kLanes >= 16 ? 16 : kThreads / kLanes >= 8 ? 8 : 4;
+  constexpr int kLanes = C::kDim / 4, kSets = kThreads / kLanes;
   static_assert(kMaxShares * 8 + kSets * kLanes * 16 <= C::kSmem, "the rings' memory is free by now");
   float2* s_ml = reinterpret_cast<float2*>(smem);                          // [parts]: maximum and sum, then the weight
   float4* s_v = reinterpret_cast<float4*>(smem + kMaxShares * 8);          // [kSets][kLanes]
@@ -918,7 +922,7 @@ cudaError_t launch(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream
   static_assert(C::kSmem + 6144 <= 232448, "with what else a block holds in shared memory");
   static_assert(C::kRows <= C::kPartRows && 4 * NT <= C::kPartRows && C::kHalf % 16 == 0 && C::kStages >= 1, "layout");
   if (!a.q) return cudaFuncSetAttribute(k_kv_attend<G, T, L, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
-  k_kv_attend<G, T, L, NT><<<kGrid, kThreads, C::kSmem, stream>>>(s, a, ctl);
+  k_kv_attend<G, T, L, NT><<<kGrid, C::kThreads, C::kSmem, stream>>>(s, a, ctl);
   return cudaGetLastError();
 }
 
