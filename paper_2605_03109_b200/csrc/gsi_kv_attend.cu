@@ -401,7 +401,9 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           *to = __float2half_rn(hi * odd);
           if constexpr (T == 2) to[32] = __float2half_rn(lo * odd);   // the next column: 4 lanes of 16 bytes on
         }
-        if (lane == 0) s_factor[r] = fminf(fmaxf(a.scale / k0 * (0x1p24f / k1), -0x1p100f), 0x1p100f);
+        // (powers of two: 2^(24 - k) in two steps)
+        const float back0 = __uint_as_float((uint32_t)(127 - k / 2) << 23), back1 = __uint_as_float((uint32_t)(151 - k + k / 2) << 23);
+        if (lane == 0) s_factor[r] = fminf(fmaxf(a.scale * back0 * back1, -0x1p100f), 0x1p100f);
       }
       __syncwarp();
       // Per block, what the scores' sums begin with, -8 times the sum of the column's q (the sums are then those of
@@ -856,60 +858,68 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
     }
   }
 
-  // ---- segments that many warps share, by the block of the last of them: its threads take four channels each of
-  // every kSets-th part
+  // ---- segments that many warps share, by the block of the last of them: its threads take four channels each,
+  // of every part or, few rows, of one part in `sets`;
   __syncthreads();
-  constexpr int kLanes = C::kDim / 4, kSets = kThreads / kLanes;
-  static_assert(kMaxShares * 8 + kSets * kLanes * 16 <= C::kSmem, "the rings' memory is free by now");
-  float2* s_ml = reinterpret_cast<float2*>(smem);                          // [parts]: maximum and sum, then the weight
-  float4* s_v = reinterpret_cast<float4*>(smem + kMaxShares * 8);          // [kSets][kLanes]
-  __shared__ float s_red[kWarps];
-  const int n_pending = s_n_pending, set = tid / kLanes, c4 = tid - set * kLanes;
+  // as many rows at a time as their weights have room for.
+  constexpr int kLanes = C::kDim / 4, kWeights = 8192;
+  static_assert(kWeights * 8 + kThreads * 16 + kMaxRows * 4 <= C::kSmem && kWeights >= kMaxShares, "the rings' memory is free by now");
+  float2* s_ml = reinterpret_cast<float2*>(smem);                                     // [rows][parts]: maximum and sum, then the weight
+  float4* s_v = reinterpret_cast<float4*>(smem + kWeights * 8);                       // [sets][rows][kLanes]
+  float* s_all = reinterpret_cast<float*>(smem + kWeights * 8 + kThreads * 16);       // [rows]
+  const int n_pending = s_n_pending;
   for (int i = 0; i < n_pending; ++i) {
     const Pending& x = s_pending[i];
     auto part_of = [&](int y) { return a.parts + (2ll * (x.first + y) + (y == 0)) * C::kPart; };
-    for (int r = 0; r < x.rows; ++r) {
-      float top = kNone, all = 0.f;
-      for (int y = tid; y < x.parts; y += kThreads) {
-        s_ml[y] = __ldcg(reinterpret_cast<const float2*>(part_of(y) + C::kPartRows * C::kDim) + r);
-        top = fmaxf(top, s_ml[y].x);
+    const int at_once = min(x.rows, max(1, kWeights / x.parts));
+    for (int r0 = 0; r0 < x.rows; r0 += at_once) {
+      const int rows = min(at_once, x.rows - r0), n = rows * kLanes, sets = max(1, kThreads / n);
+      for (int e = tid; e < rows * x.parts; e += kThreads) {
+        const int r = e / x.parts, y = e - r * x.parts;
+        s_ml[e] = __ldcg(reinterpret_cast<const float2*>(part_of(y) + C::kPartRows * C::kDim) + r0 + r);
       }
-#pragma unroll
-      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      if (lane == 0) s_red[warp] = top;
       __syncthreads();
+      for (int r = warp; r < rows; r += kWarps) {
+        float top = kNone, all = 0.f;
+        for (int y = lane; y < x.parts; y += 32) top = fmaxf(top, s_ml[r * x.parts + y].x);
 #pragma unroll
-      for (int y = 0; y < kWarps; ++y) top = fmaxf(top, s_red[y]);
-      for (int y = tid; y < x.parts; y += kThreads) {
-        const float f = exp2_fast(s_ml[y].x - top);
-        all += s_ml[y].y * f;
-        s_ml[y].x = f;
-      }
-      all = warp_sum(all);
-      __syncthreads();
-      if (lane == 0) s_red[warp] = all;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (set < kSets) {
-#pragma unroll 8
-        for (int y = set; y < x.parts; y += kSets) {
-          const float4 w = __ldcg(reinterpret_cast<const float4*>(part_of(y) + r * C::kDim) + c4);
-          const float f = s_ml[y].x;
-          v.x += w.x * f, v.y += w.y * f, v.z += w.z * f, v.w += w.w * f;
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        for (int y = lane; y < x.parts; y += 32) {
+          float2& ml = s_ml[r * x.parts + y];
+          ml.x = exp2_fast(ml.x - top);
+          all += ml.y * ml.x;
         }
-        s_v[set * kLanes + c4] = v;
+        all = warp_sum(all);
+        if (lane == 0) s_all[r] = all;
       }
       __syncthreads();
-      if (set == 0) {
-        float sums[4] = {0.f, 0.f, 0.f, 0.f};
-        all = 0.f;
-#pragma unroll
-        for (int y = 0; y < kWarps; ++y) all += s_red[y];
-        for (int y = 0; y < kSets; ++y) {
-          const float4 w = s_v[y * kLanes + c4];
-          sums[0] += w.x, sums[1] += w.y, sums[2] += w.z, sums[3] += w.w;
+      for (int e0 = 0; e0 < n; e0 += kThreads) {   // (once, but where a set is more than the block's threads)
+        const int set = n >= kThreads ? 0 : tid / n, e = e0 + tid - set * n, r = e / kLanes, c4 = e - r * kLanes;
+        const bool mine = set < sets && e < n;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (mine) {
+#pragma unroll 16
+          for (int y = set; y < x.parts; y += sets) {
+            const float4 w = __ldcg(reinterpret_cast<const float4*>(part_of(y) + (r0 + r) * C::kDim) + c4);
+            const float f = s_ml[r * x.parts + y].x;
+            v.x += w.x * f, v.y += w.y * f, v.z += w.z * f, v.w += w.w * f;
+          }
         }
-        for (int e = 0; e < 4; ++e)
-          if (c4 * 4 + e < s.head_dim) store_from_float(a.out, a.dtype, x.out[r] + c4 * 4 + e, all == 0.f ? 0.f : sums[e] / all);
+        if (sets > 1) {
+          if (mine) s_v[set * n + e] = v;
+          __syncthreads();
+          if (mine && set == 0)
+            for (int y = 1; y < sets; ++y) {
+              const float4 w = s_v[y * n + e];
+              v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+            }
+        }
+        if (mine && set == 0) {
+          const float all = s_all[r], sums[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (c4 * 4 + k < s.head_dim) store_from_float(a.out, a.dtype, x.out[r0 + r] + c4 * 4 + k, all == 0.f ? 0.f : sums[k] / all);
+        }
       }
       __syncthreads();
     }
