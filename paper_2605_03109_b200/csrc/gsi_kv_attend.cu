@@ -57,9 +57,13 @@ struct Cfg {
   static constexpr int kHalf = G * kBlockBytes;        // K of a tile, or V
   static constexpr int kStages = (kWarps == 16 ? 9216 : 14336) / (2 * kHalf) / kTiles;   // units under way
   static constexpr int kRing = kStages * kTiles * 2 * kHalf;
+  // A tile comes in one copy; where only one unit has room, in two, so that K of the next one comes while V is read.
+  static constexpr bool kSplit = kStages == 1;
+  static constexpr int kStride = kSplit ? kHalf : 2 * kHalf;      // from tile to tile
+  static constexpr int kToV = kSplit ? kTiles * kHalf : kHalf;    // from a tile's K to its V
   static constexpr int kQ = NT * G * 1024;
   static constexpr int kSums = ((3 * G + 1) * kRows * 4 + 15) / 16 * 16;   // per block: -8 times the sums of q's terms, the sum of q; factors
-  static constexpr int kBars = kStages * 2 * 8;
+  static constexpr int kBars = kStages * (kSplit ? 2 : 1) * 8;
   static constexpr int kWarpBytes = (kRing + kQ + kSums + kBars + 15) / 16 * 16;
   static constexpr int kSmem = kWarps * kWarpBytes;
   static_assert(kShares <= kMaxShares, "the workspace's parts and tickets");
@@ -118,7 +122,7 @@ __device__ __forceinline__ uint32_t centred(uint32_t w) {
   else h = __hadd2(h, __half2half2(__ushort_as_half(0xE408)));   // - 1032
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ void copy_half(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint64_t policy) {
+__device__ __forceinline__ void copy_tile(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint64_t policy) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
                "l"(src), "r"(bytes), "r"(bar), "l"(policy)
                : "memory");
@@ -189,17 +193,16 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
   __shared__ Pending s_pending[kWarps * 2];
   __shared__ int s_n_pending;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gr = lane >> 2, t4 = lane & 3;
-  unsigned char* ring_k = smem + warp * C::kWarpBytes;
-  unsigned char* ring_v = ring_k + C::kRing / 2;
-  unsigned char* s_q = ring_k + C::kRing;
+  unsigned char* ring = smem + warp * C::kWarpBytes;
+  unsigned char* s_q = ring + C::kRing;
   float* s_start = reinterpret_cast<float*>(s_q + C::kQ);   // [G][kRows][2]
   float* s_sum = s_start + 2 * G * C::kRows;                // [G][kRows]
   float* s_factor = s_sum + G * C::kRows;                   // [kRows]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(s_q + C::kQ + C::kSums);   // of K, then of V
+  uint64_t* bars = reinterpret_cast<uint64_t*>(s_q + C::kQ + C::kSums);   // of the stages (K, then V, where they come apart)
   auto load = [&](int i) { return load_seq<C::kRows, N>(s, a, i); };
 
   if (lane == 0)
-    for (int i = 0; i < 2 * C::kStages; ++i) mbar_init(bars + i, N);
+    for (int i = 0; i < C::kBars / 8; ++i) mbar_init(bars + i, N);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   if (tid == 0) s_n_pending = 0;
 
@@ -298,7 +301,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
       fetch(q_from(q, head, step0, row0 - step0 * a.shared, 0), q_first);
     }
 
-    // ---- its tiles come through two rings, K and V; lane (N j + i) % 32 knows where tile i of unit j lies
+    // ---- its tiles come through a ring; lane (N j + i) % 32 knows where tile i of unit j lies
     int look_seq = seq;
     long long look_base = base;
     const unsigned char* where = nullptr;
@@ -340,20 +343,19 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
       q_at[i] = s32(s_q) + ((N == 1 || of ? gr % (2 * L) : 2 * L) * 4 + t4) * 16;
     }
     const int my_tile = t4 / L;   // the one whose scores this lane has
-    const uint32_t k_ring = s32(ring_k), v_ring = s32(ring_v), start_at = s32(s_start), sum_at = s32(s_sum);
-    const uint32_t my_pair = my_tile * C::kHalf + kCodeBytes + gr * 8, my_codes = lane * 16;
-    const uint32_t my_k = k_ring + lane % N * C::kHalf, my_v = v_ring + lane % N * C::kHalf;   // where its copies go, and their barriers
-    const uint32_t my_bar = s32(bars);
+    const uint32_t ring_at = s32(ring), start_at = s32(s_start), sum_at = s32(s_sum);
+    const uint32_t my_pair = my_tile * C::kStride + kCodeBytes + gr * 8, my_codes = lane * 16;
+    const uint32_t my_slot = ring_at + lane % N * C::kStride, my_bar = s32(bars);   // where its copies go, and their barriers
     const uint64_t policy = L == 4 ? as_usual() : first_out();   // (many rows: other units read the same tiles)
     auto row_of = [&](int n, int r) { return T == 2 ? n * L + t4 % L : n * 2 * L + t4 % L * 2 + r; };
 
-    // K (V) of unit j, if there is one, to its stage
+    // unit j, if there is one, to its stage (its K or its V, where they come apart)
     auto issue = [&](int j, int stage, bool of_v) {
       if (j < mine && lane / N == j % (32 / N)) {
-        const uint32_t bar = my_bar + ((of_v ? C::kStages : 0) + stage) * 8;
+        const uint32_t bar = my_bar + (stage + of_v) * 8;
         if (where) {
-          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(C::kHalf) : "memory");
-          copy_half((of_v ? my_v : my_k) + stage * N * C::kHalf, where + (of_v ? C::kHalf : 0), C::kHalf, bar, policy);
+          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(C::kStride) : "memory");
+          copy_tile(my_slot + (C::kSplit ? of_v * C::kToV : stage * N * C::kStride), where + of_v * C::kHalf, C::kStride, bar, policy);
         } else {
           asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
         }
@@ -361,7 +363,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
     };
     if (mine > 0) look_up(0);
 #pragma unroll 1
-    for (int i = 0; i < 2 * C::kStages; ++i) issue(i >> 1, i >> 1, i & 1);
+    for (int i = 0; i < C::kBars / 8; ++i) issue(C::kSplit ? 0 : i, C::kSplit ? 0 : i, C::kSplit && i);
 
     // ---- segments of the share
     for (int j = 0; j < mine && !gave_up;) {
@@ -485,7 +487,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
         const int pos = first_pos + my_tile * kTile + gr;
         const bool wrong = kMasked && (missing >> my_tile & 1u);
         float S[NT][kLR][2], p[NT][kLR][2];
-        const uint32_t k_at = k_ring + stage * N * C::kHalf, v_at = v_ring + stage * N * C::kHalf;
+        const uint32_t k_at = ring_at + stage * N * C::kStride, v_at = k_at + C::kToV;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
           const uint2 pw = lds64(k_at + my_pair + g * kBlockBytes);
@@ -504,7 +506,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           }
 #pragma unroll
           for (int i = 0; i < N; ++i) {
-            const uint4 w = lds128(k_at + my_codes + (i * C::kHalf + g * kBlockBytes));
+            const uint4 w = lds128(k_at + my_codes + (i * C::kStride + g * kBlockBytes));
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const uint32_t x = h ? w.y : w.x, y = h ? w.w : w.z;
@@ -529,11 +531,13 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
               S[n][r][1] = fmaf(p1.x, a1, g ? fmaf(p1.y, qs, S[n][r][1]) : p1.y * qs);
             }
         }
-        __syncwarp();
-        issue(next, stage, false);
-        if (__any_sync(0xffffffffu, !mbar_wait(bars + C::kStages + stage, phase))) {
-          gave_up = true;
-          return;
+        if constexpr (C::kSplit) {
+          __syncwarp();
+          issue(next, 0, false);
+          if (__any_sync(0xffffffffu, !mbar_wait(bars + 1, phase))) {
+            gave_up = true;
+            return;
+          }
         }
         // pairs of V, and their largest step
         uint2 pv[G];
@@ -644,7 +648,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           }
 #pragma unroll
           for (int i = 0; i < N; ++i) {
-            const uint4 w = lds128(v_at + my_codes + (i * C::kHalf + g * kBlockBytes));
+            const uint4 w = lds128(v_at + my_codes + (i * C::kStride + g * kBlockBytes));
             const uint32_t x8 = w.x >> 8, y8 = w.y >> 8, z8 = w.z >> 8, w8 = w.w >> 8;
             const uint32_t A[4][4] = {{centred<false>(w.x), centred<false>(w.y), centred<false>(w.z), centred<false>(w.w)},
                                       {centred<true>(w.x), centred<true>(w.y), centred<true>(w.z), centred<true>(w.w)},
@@ -696,13 +700,13 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           pass(std::false_type{}, pos, 0u, j + C::kStages);
         } else if (pos < most) {
           pass(std::true_type{}, pos, missing, j + C::kStages);
-        } else {
-          issue(j + C::kStages, stage, false);
-          if (__any_sync(0xffffffffu, !mbar_wait(bars + C::kStages + stage, phase))) gave_up = true;
+        } else if constexpr (C::kSplit) {
+          issue(j + 1, 0, false);
+          if (__any_sync(0xffffffffu, !mbar_wait(bars + 1, phase))) gave_up = true;
         }
-        if (gave_up) break;
+        if (C::kSplit && gave_up) break;
         __syncwarp();
-        issue(j + C::kStages, stage, true);
+        issue(j + C::kStages, stage, C::kSplit);
         if (++stage == C::kStages) {
           stage = 0;
           phase ^= 1u;
@@ -849,7 +853,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
       // (copies in flight land before the block's memory is another's)
       for (int i = 0; i < C::kStages; ++i) {
         mbar_wait(bars + stage, phase);
-        mbar_wait(bars + C::kStages + stage, phase);
+        if (C::kSplit) mbar_wait(bars + 1, phase);
         if (++stage == C::kStages) {
           stage = 0;
           phase ^= 1u;
