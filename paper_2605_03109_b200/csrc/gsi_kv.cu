@@ -1,5 +1,6 @@
 // A cache of keys and values in 4 bits: handles and argument checks, tables and slot maps from the requests'
 // lengths, new rows into the pages and back.  The attention over them is gsi_kv_attend.cu.
+#include <climits>
 #include <cmath>
 #include <new>
 
@@ -11,11 +12,12 @@ namespace kv {
 namespace {
 
 constexpr int kPlanThreads = 512;
-constexpr int kPlanTokens = 4 * kPlanThreads;   // slots of a block in one round
-constexpr int kPlanGrid = 296;
+constexpr int kRun = 8;   // slots of a thread in one round
+constexpr int kPlanGrid = 444;
 
 __device__ __forceinline__ int clamp_int(long long v) { return v > 0x7fffffffll ? 0x7fffffff : (int)v; }
-__device__ __forceinline__ int pages_of(long long tokens, int page_tokens) { return (int)((tokens + page_tokens - 1) / page_tokens); }
+// (up to 2^31 tokens and a page)
+__device__ __forceinline__ int pages_of(long long tokens, int page_tokens) { return (int)(((unsigned)tokens + page_tokens - 1) / (unsigned)page_tokens); }
 
 // The last index s with first[s] <= i (first[0] <= i, ascending).
 __device__ __forceinline__ int last_at_most(const int* first, int n, int i) {
@@ -41,9 +43,9 @@ __device__ __forceinline__ bool read_last(Control* ctl, int* s_last) {
 }
 
 // Every block works the requests' sums out for itself (2048 requests: 16 KB from the L2), so that no block waits for
-// another; the sequences' first rows and first pages stay in shared memory, where each token and page of the block
-// looks up its own.  The block that is last to have read the state moves it on.
-// Bound by the launch and three dependent reads; by the writes of slots and positions for prompts.
+// another; the sequences' first rows and first pages stay in shared memory, where each run of tokens and each page of the
+// block looks up its own.  The block that is last to have read the state moves it on.
+// Bound by the launch and three dependent reads (one token: 4.1 us a call); for prompts by the writes of slots and positions.
 __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, Control* ctl) {
   extern __shared__ int sm[];
   int* s_row = sm;                    // first row of a sequence
@@ -51,40 +53,45 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
   int* s_len = s_page + a.n_seqs;     // its tokens so far; -1: refused
   __shared__ Scan2 s_warp[kPlanThreads / 32];
   __shared__ int s_last, s_took, s_refused;
+  const int threads = blockDim.x;
   if (threadIdx.x == 0) s_took = s_refused = 0;
+  pdl_launch_dependents();
+  pdl_wait();
   const int n_free = min(max(*a.n_free, 0), s.n_pages);
-  const int per = (a.n_seqs + kPlanThreads - 1) / kPlanThreads, first = threadIdx.x * per, last = min(first + per, a.n_seqs);
+  const int per = (a.n_seqs + threads - 1) / threads, first = threadIdx.x * per, last = min(first + per, a.n_seqs);
   const long long room = (long long)s.max_pages * s.page_tokens;
-  // (rows of a sequence come first, whether it can be longer follows from where they end)
+  auto need_of = [&](int len, int add) { return pages_of((long long)len + add, s.page_tokens) - pages_of(len, s.page_tokens); };
+  auto fits = [&](int len, int add) { return add >= 0 && len >= 0 && (long long)len + add <= room; };
   Scan2 sum{0, 0}, total;
-  for (int i = first; i < last; ++i) sum.a += max(__ldg(a.n_new + i), 0);
-  Scan2 at = block_scan(sum, &total, s_warp);
-  const long long n_rows = total.a;
-  long long row = at.a;
-  auto fits = [&](int len, int add, long long end) {
-    return add >= 0 && len >= 0 && (long long)len + add <= room && end <= s.max_tokens;
-  };
-  sum = {0, 0};
   for (int i = first; i < last; ++i) {
     const int len = a.lens[i], add = __ldg(a.n_new + i);
-    row += max(add, 0);
-    if (fits(len, add, row)) sum.b += pages_of((long long)len + add, s.page_tokens) - pages_of(len, s.page_tokens);
+    sum.a += max(add, 0);
+    if (fits(len, add)) sum.b += need_of(len, add);
   }
-  Scan2 got = block_scan(sum, &total, s_warp);
-  row = at.a;
-  long long asked = got.b;
+  Scan2 at = block_scan(sum, &total, s_warp);
+  const long long n_rows = total.a;
+  if (n_rows > s.max_tokens) {   // (those whose rows end behind the slots ask for nothing)
+    long long row = at.a;
+    sum.b = 0;
+    for (int i = first; i < last; ++i) {
+      const int len = a.lens[i], add = __ldg(a.n_new + i);
+      row += max(add, 0);
+      if (fits(len, add) && row <= s.max_tokens) sum.b += need_of(len, add);
+    }
+    at.b = block_scan(sum, &total, s_warp).b;
+  }
   int took = 0, refused = 0;
   for (int i = first; i < last; ++i) {
     const int len = a.lens[i], add = __ldg(a.n_new + i);
-    s_row[i] = clamp_int(row);
-    s_page[i] = clamp_int(asked);
-    row += max(add, 0);
-    bool ok = fits(len, add, row);
+    s_row[i] = clamp_int(at.a);
+    s_page[i] = clamp_int(at.b);
+    at.a += max(add, 0);
+    bool ok = fits(len, add) && at.a <= s.max_tokens;
     if (ok) {
-      const int need = pages_of((long long)len + add, s.page_tokens) - pages_of(len, s.page_tokens);
-      asked += need;
-      ok = need == 0 || asked <= n_free;
-      if (ok && need) took = (int)asked;
+      const int need = need_of(len, add);
+      at.b += need;
+      ok = need == 0 || at.b <= n_free;
+      if (ok && need) took = (int)at.b;
     }
     refused += !ok;
     s_len[i] = ok ? len : -1;
@@ -103,39 +110,62 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
     a.counts[2] = n_free - s_took;
     a.counts[3] = s_refused;
   }
-  // slots and positions, four tokens a thread
-  for (long long i0 = (long long)blockIdx.x * kPlanTokens + threadIdx.x * 4; i0 < s.max_tokens; i0 += (long long)gridDim.x * kPlanTokens) {
-    int slot[4], pos[4];
-    int q = i0 < n_rows ? last_at_most(s_row, a.n_seqs, (int)i0) : 0;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      slot[u] = pos[u] = -1;
-      const long long i = i0 + u;
-      if (i >= n_rows || i >= s.max_tokens) continue;
-      while (q + 1 < a.n_seqs && s_row[q + 1] <= i) ++q;
-      const int len = s_len[q];
-      if (len < 0) continue;
-      const int p = len + (int)(i - s_row[q]), index = p / s.page_tokens, held = pages_of(len, s.page_tokens);
-      const int page = index < held ? a.table[(long long)q * s.max_pages + index] : __ldg(a.free_pages + (n_free - 1 - (s_page[q] + index - held)));
-      if ((unsigned)page >= (unsigned)s.n_pages) {
-        ctl->status = GSI_ERR_INVALID_ARG;
-        continue;
-      }
-      pos[u] = p;
-      slot[u] = page * s.page_tokens + (p - index * s.page_tokens);
+  // slots and positions, a run of tokens a thread: its sequence is looked up once, a page where it changes
+  const bool vec = ((reinterpret_cast<uintptr_t>(a.slots) | reinterpret_cast<uintptr_t>(a.positions)) & 15) == 0;
+  for (long long i0 = ((long long)blockIdx.x * threads + threadIdx.x) * kRun; i0 < s.max_tokens; i0 += (long long)gridDim.x * threads * kRun) {
+    int slot[kRun], pos[kRun];
+    int q = 0, len = -1, p = 0, behind = 0, base = 0, left = 0;   // tokens of the sequence, of the page, that are left
+    if (i0 < n_rows) {
+      q = last_at_most(s_row, a.n_seqs, (int)i0);
+      behind = (q + 1 < a.n_seqs ? s_row[q + 1] : clamp_int(n_rows)) - (int)i0;
+      len = s_len[q];
+      p = len + (int)i0 - s_row[q];
     }
-    if (i0 + 4 <= s.max_tokens && (reinterpret_cast<uintptr_t>(a.slots) & 15) == 0 && (reinterpret_cast<uintptr_t>(a.positions) & 15) == 0) {
-      *reinterpret_cast<int4*>(a.slots + i0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
-      *reinterpret_cast<int4*>(a.positions + i0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-    } else {
-      for (int u = 0; u < 4 && i0 + u < s.max_tokens; ++u) {
-        a.slots[i0 + u] = slot[u];
-        a.positions[i0 + u] = pos[u];
+#pragma unroll
+    for (int u = 0; u < kRun; ++u) {
+      slot[u] = pos[u] = -1;
+      if (i0 + u >= n_rows) continue;
+      if (behind == 0) {
+        do {
+          ++q;
+          behind = (q + 1 < a.n_seqs ? s_row[q + 1] : clamp_int(n_rows)) - s_row[q];
+        } while (behind == 0);
+        len = p = s_len[q];
+        left = 0;
       }
+      --behind;
+      if (len < 0) continue;
+      if (left == 0) {
+        const int index = p / s.page_tokens, held = pages_of(len, s.page_tokens);
+        const int page = index < held ? a.table[(long long)q * s.max_pages + index] : __ldg(a.free_pages + (n_free - 1 - (s_page[q] + index - held)));
+        base = (unsigned)page < (unsigned)s.n_pages ? (page - index) * s.page_tokens : INT_MIN;
+        left = (index + 1) * s.page_tokens - p;
+        if (base == INT_MIN) ctl->status = GSI_ERR_INVALID_ARG;
+      }
+      if (base != INT_MIN) {
+        pos[u] = p;
+        slot[u] = base + p;
+      }
+      ++p;
+      --left;
+    }
+    if (vec && i0 + kRun <= s.max_tokens) {
+#pragma unroll
+      for (int u = 0; u < kRun; u += 4) {
+        *reinterpret_cast<int4*>(a.slots + i0 + u) = make_int4(slot[u], slot[u + 1], slot[u + 2], slot[u + 3]);
+        *reinterpret_cast<int4*>(a.positions + i0 + u) = make_int4(pos[u], pos[u + 1], pos[u + 2], pos[u + 3]);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kRun; ++u)
+        if (i0 + u < s.max_tokens) {
+          a.slots[i0 + u] = slot[u];
+          a.positions[i0 + u] = pos[u];
+        }
     }
   }
   // the new pages
-  for (int j = blockIdx.x * kPlanThreads + threadIdx.x; j < s_took; j += gridDim.x * kPlanThreads) {
+  for (int j = blockIdx.x * threads + threadIdx.x; j < s_took; j += gridDim.x * threads) {
     const int q = last_at_most(s_page, a.n_seqs, j);
     a.table[(long long)q * s.max_pages + pages_of(s_len[q], s.page_tokens) + j - s_page[q]] = __ldg(a.free_pages + (n_free - 1 - j));
   }
@@ -152,6 +182,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_release(Shape s, ReleaseArg
   int* s_page = sm;   // pages that the sequences before give back
   __shared__ Scan2 s_warp[kPlanThreads / 32];
   __shared__ int s_last;
+  pdl_launch_dependents();
+  pdl_wait();
   const int n_free = min(max(*a.n_free, 0), s.n_pages);
   const int per = (a.n_seqs + kPlanThreads - 1) / kPlanThreads, first = threadIdx.x * per, last = min(first + per, a.n_seqs);
   auto held = [&](int i) { return a.done[i] ? min(pages_of(max(a.lens[i], 0), s.page_tokens), s.max_pages) : 0; };
@@ -179,40 +211,74 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_release(Shape s, ReleaseArg
   if (threadIdx.x == 0) *a.n_free = n_free + n;
 }
 
-// Sixteen channels of a row from `channel` on; those from head_dim on are 0.
-template <bool kVec>
-__device__ __forceinline__ void load16(const void* base, gsi_dtype_t dtype, long long at, int n, float (&x)[16]) {
-  if (kVec && n >= 16) {
-    if (dtype == GSI_F32) {
-      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
+__device__ __forceinline__ float min_nan(float a, float b) {   // (NaN where one is)
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// Two 16-bit values of a word.
+template <gsi_dtype_t kType>
+__device__ __forceinline__ float2 pair_of(uint32_t w) {
+  if constexpr (kType == GSI_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+  else return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+
+// Channels 4 t + 16 i .. + 3 of a row, i = 0..3, as lane quarter t takes them (four lanes read 64 or 32 bytes in one go); those
+// from n on repeat channel 0 of `at`, which changes neither bound.
+template <gsi_dtype_t kType, bool kVec>
+__device__ __forceinline__ void load_quarters(const void* base, long long at, int t, int n, float (&x)[16]) {
+  if (kVec && n >= kGroup) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 v = __ldg(p + i);
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (kType == GSI_F32) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(base) + at) + 4 * i + t);
         x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
-      }
-    } else {
-      const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint4 v = __ldg(p + i);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (dtype == GSI_BF16) {
-            x[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-            x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-          } else {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-            x[8 * i + 2 * j] = f.x;
-            x[8 * i + 2 * j + 1] = f.y;
-          }
-        }
+      } else {
+        const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + at) + 4 * i + t);
+        const float2 a = pair_of<kType>(v.x), b = pair_of<kType>(v.y);
+        x[4 * i] = a.x, x[4 * i + 1] = a.y, x[4 * i + 2] = b.x, x[4 * i + 3] = b.y;
       }
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = i < n ? load_as_float(base, dtype, at + i) : 0.f;
+    for (int i = 0; i < 16; ++i) {
+      const int c = i / 4 * 16 + t * 4 + i % 4;
+      x[i] = load_as_float(base, kType, at + (c < n ? c : 0));
+    }
   }
+}
+
+// rint((x - mid) / step) of the four channels c .. c + 3 as signed nibbles.  The quotient, a single fp32 division, is only
+// taken where the product with 1 / step, which is off by 2^-22 of it at most, lies near a border.
+__device__ __forceinline__ uint32_t nibbles4(const float* x, float mid, float step, float inverse) {
+  uint32_t got = 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float d = __fsub_rn(x[i], mid);
+    float r = fminf(fmaxf(d * inverse, -8.f), 7.f);
+    float k = __fadd_rn(r, 12582912.f);   // 1.5 x 2^23: its last bits are the whole number
+    if (fabsf(r - __fsub_rn(k, 12582912.f)) > 0.4999f) k = __fadd_rn(fminf(fmaxf(__fdiv_rn(d, step), -8.f), 7.f), 12582912.f);
+    got |= (__float_as_uint(k) & 15u) << 4 * i;
+  }
+  return got;
+}
+
+// Of four lanes (quarters t of a row), each with four 16-bit pieces h[i] of piece group i: lane t gets group t's four, in
+// lane order.
+__device__ __forceinline__ uint2 transpose4(uint32_t h0, uint32_t h1, uint32_t h2, uint32_t h3, int t) {
+  const uint32_t low = h0 | h1 << 16, high = h2 | h3 << 16;
+  const uint32_t far = __shfl_xor_sync(0xffffffffu, (t & 2) ? low : high, 2);
+  const uint32_t a = (t & 2) ? far : low, b = (t & 2) ? high : far;    // groups (t & 2) + 0, 1 of lanes t & 1 and (t & 1) + 2
+  const uint32_t send = (t & 1) ? __byte_perm(a, b, 0x5410) : __byte_perm(a, b, 0x7632);
+  const uint32_t keep = (t & 1) ? __byte_perm(a, b, 0x7632) : __byte_perm(a, b, 0x5410);
+  const uint32_t got = __shfl_xor_sync(0xffffffffu, send, 1);
+  const uint32_t first = (t & 1) ? got : keep, second = (t & 1) ? keep : got;   // of lanes 0 and 2, of lanes 1 and 3
+  return make_uint2(__byte_perm(first, second, 0x5410), __byte_perm(first, second, 0x7632));
 }
 
 // A warp takes eight tokens of one head, K or V, 64 channels: four lanes a token, sixteen channels a lane.
@@ -238,9 +304,12 @@ __device__ __forceinline__ unsigned char* block_of(const Shape& s, unsigned char
   return pages + tile_at(s, page, it.head, in / kTile) + (it.is_v * s.groups + it.group) * kBlockBytes;
 }
 
-template <bool kVec>
+// Bound by the rows' bytes for long prompts, where 64 channels of a token cost four lanes about 70 instructions each.
+template <gsi_dtype_t kType, bool kVec>
 __global__ void __launch_bounds__(256) k_kv_append(Shape s, RowsArgs a, Control* ctl) {
-  const int lane = threadIdx.x & 31, quarter = lane & 3;
+  const int quarter = threadIdx.x & 3;
+  pdl_launch_dependents();
+  pdl_wait();
   for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < items(s, a.n); w += (long long)gridDim.x * 8) {
     const Item it = item_of(s, a.n, w);
     int slot = it.row < a.n ? __ldg(a.slots + it.row) : -1;
@@ -248,112 +317,115 @@ __global__ void __launch_bounds__(256) k_kv_append(Shape s, RowsArgs a, Control*
       ctl->status = GSI_ERR_INVALID_ARG;
       slot = -1;
     }
-    const int c = it.group * kGroup + quarter * 16, n = min(s.head_dim - c, 16);   // (n <= 0: no channel of this lane)
     float x[16];
-    float lo = INFINITY, hi = -INFINITY;
-    bool finite = true;
-    if (slot >= 0 && n > 0)
-      load16<kVec>(it.is_v ? a.v : a.k, a.dtype, it.row * (it.is_v ? a.v_token : a.k_token) + it.head * (it.is_v ? a.v_head : a.k_head) + c, n, x);
-    else
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    if (slot >= 0)
+      load_quarters<kType, kVec>(it.is_v ? a.v : a.k, it.row * (it.is_v ? a.v_token : a.k_token) + it.head * (it.is_v ? a.v_head : a.k_head) + it.group * kGroup,
+                                 quarter, s.head_dim - it.group * kGroup, x);
+    float lo = x[0], hi = x[0];
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i < n) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-        finite = finite && fabsf(x[i]) <= 3.402823466e38f;
-      }
-    int all = finite;
+    for (int i = 1; i < 16; ++i) {
+      lo = min_nan(lo, x[i]);
+      hi = max_nan(hi, x[i]);
+    }
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
-      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-      all &= __shfl_xor_sync(0xffffffffu, all, o);
+      lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
+    const bool finite = lo >= -3.402823466e38f && hi <= 3.402823466e38f;   // (false for NaN)
     const __half s16 = __float2half_rn(fminf(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), 65504.f));
     const float step = __half2float(s16);
     const __half m16 = __float2half_rn(fminf(fmaxf(__fadd_rn(lo, 8.f * step), -65504.f), 65504.f));
-    const float mid = __half2float(m16);
-    uint32_t code[2] = {0u, 0u};
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float v = step == 0.f ? 8.f : __fadd_rn(rintf(__fdiv_rn(__fsub_rn(x[i], mid), step)), 8.f);
-      v = fminf(fmaxf(v, 0.f), 15.f);
-      code[i >> 3] |= (all && i < n ? (uint32_t)v : 0u) << 4 * (i & 7);
-    }
+    const float mid = __half2float(m16), inverse = step == 0.f ? 0.f : __fdividef(1.f, step);
+    uint2 code = transpose4(nibbles4(x, mid, step, inverse), nibbles4(x + 4, mid, step, inverse), nibbles4(x + 8, mid, step, inverse),
+                            nibbles4(x + 12, mid, step, inverse), quarter);
+    code.x = step == 0.f ? 0x88888888u : code.x ^ 0x88888888u;   // (8 where there is no step)
+    code.y = step == 0.f ? 0x88888888u : code.y ^ 0x88888888u;
+    if (!finite) code = make_uint2(0u, 0u);
     int t = 0;
     unsigned char* block = slot >= 0 ? block_of(s, a.pages, slot, it, &t) : nullptr;
     // V: a word is four channels of a pair of tokens; where the neighbouring lanes hold the other token of the pair,
     // each writes one of their two octets of channels whole
     const int other = __shfl_xor_sync(0xffffffffu, slot, 4);
-    const uint32_t far[2] = {__shfl_xor_sync(0xffffffffu, code[0], 4), __shfl_xor_sync(0xffffffffu, code[1], 4)};
+    const uint2 far = make_uint2(__shfl_xor_sync(0xffffffffu, code.x, 4), __shfl_xor_sync(0xffffffffu, code.y, 4));
     if (!block) continue;
     if (quarter == 0) {
-      const __half2 pair = all ? __halves2half2(s16, m16) : __half2half2(__ushort_as_half(0x7FFF));
+      const __half2 pair = finite ? __halves2half2(s16, m16) : __half2half2(__ushort_as_half(0x7FFF));
       *reinterpret_cast<__half2*>(block + pair_byte(t)) = pair;
     }
     if (!it.is_v) {
-      *reinterpret_cast<uint2*>(block + k_byte(t, quarter * 16)) = make_uint2(code[0], code[1]);
+      *reinterpret_cast<uint2*>(block + k_byte(t, quarter * 16)) = code;
     } else if (other >= 0 && other == (slot ^ 1)) {
       const int odd = t & 1;
-      const uint32_t mine = odd ? code[1] : code[0], theirs = odd ? far[1] : far[0];
+      const uint32_t mine = odd ? code.y : code.x, theirs = odd ? far.y : far.x;
       const uint32_t even_token = odd ? theirs : mine, odd_token = odd ? mine : theirs;
       *reinterpret_cast<uint2*>(block + v_byte(t & ~1, quarter * 16 + odd * 8)) =
-          make_uint2((even_token & 0xFFFFu) | odd_token << 16, even_token >> 16 | (odd_token & 0xFFFF0000u));
+          make_uint2(__byte_perm(even_token, odd_token, 0x5410), __byte_perm(even_token, odd_token, 0x7632));
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<uint16_t*>(block + v_byte(t, quarter * 16 + i * 4)) = (uint16_t)(code[i >> 1] >> 16 * (i & 1));
+        *reinterpret_cast<uint16_t*>(block + v_byte(t, quarter * 16 + i * 4)) = (uint16_t)((i < 2 ? code.x : code.y) >> 16 * (i & 1));
     }
   }
 }
 
-template <bool kVec>
+// A lane quarter takes channels 4 t + 16 i .. + 3, so that four lanes write 64 (32) bytes in one go.
+template <gsi_dtype_t kType, bool kVec>
 __global__ void __launch_bounds__(256) k_kv_read(Shape s, RowsArgs a, Control* ctl) {
-  const int lane = threadIdx.x & 31, quarter = lane & 3;
+  const int quarter = threadIdx.x & 3;
+  pdl_launch_dependents();
+  pdl_wait();
   for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < items(s, a.n); w += (long long)gridDim.x * 8) {
     const Item it = item_of(s, a.n, w);
-    const int c = it.group * kGroup + quarter * 16, n = min(s.head_dim - c, 16);
-    if (it.row >= a.n || n <= 0) continue;
+    if (it.row >= a.n) continue;
     int slot = __ldg(a.slots + it.row);
     if (slot >= s.n_pages * s.page_tokens) {
       ctl->status = GSI_ERR_INVALID_ARG;
       slot = -1;
     }
-    float x[16];
+    int t = 0;
+    const unsigned char* block = slot >= 0 ? block_of(s, a.pages, slot, it, &t) : nullptr;
+    uint32_t codes[4] = {0u, 0u, 0u, 0u};
+    float2 pair = make_float2(0.f, 0.f);
+    if (block) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = 0.f;
-    if (slot >= 0) {
-      int t;
-      const unsigned char* block = block_of(s, a.pages, slot, it, &t);
-      uint32_t code[2];
-      if (!it.is_v) {
-        const uint2 v = *reinterpret_cast<const uint2*>(block + k_byte(t, quarter * 16));
-        code[0] = v.x;
-        code[1] = v.y;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {   // (a word of v: four channels of this token and of the other of its pair)
-          const uint2 v = *reinterpret_cast<const uint2*>(block + v_byte(t & ~1, quarter * 16 + i * 8));
-          code[i] = (t & 1) ? v.x >> 16 | (v.y & 0xFFFF0000u) : (v.x & 0xFFFFu) | v.y << 16;
-        }
+      for (int i = 0; i < 4; ++i) {
+        const int c = i * 16 + quarter * 4;
+        codes[i] = *reinterpret_cast<const uint16_t*>(block + (it.is_v ? v_byte(t, c) : k_byte(t, c)));
       }
-      const float2 pair = __half22float2(*reinterpret_cast<const __half2*>(block + pair_byte(t)));
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        x[i] = __fmaf_rn(pair.x, (float)((int)(code[i >> 3] >> 4 * (i & 7) & 15u) - 8), pair.y);   // (the product is exact)
+      pair = __half22float2(*reinterpret_cast<const __half2*>(block + pair_byte(t)));
     }
     void* to = it.is_v ? a.v : a.k;
-    const long long at = it.row * a.k_token + it.head * a.k_head + c;
-    if (kVec && n == 16 && a.dtype == GSI_F32) {
+    const long long at = it.row * a.k_token + it.head * a.k_head + it.group * kGroup;
+    const int n = s.head_dim - it.group * kGroup;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        reinterpret_cast<float4*>(static_cast<float*>(to) + at)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-    } else {
+    for (int i = 0; i < 4; ++i) {
+      const int c = i * 16 + quarter * 4;
+      float x[4];
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i < n) store_from_float(to, a.dtype, at + i, x[i]);
+      for (int k = 0; k < 4; ++k)
+        x[k] = block ? __fmaf_rn(pair.x, (float)((int)(codes[i] >> 4 * k & 15u) - 8), pair.y) : 0.f;   // (the product is exact)
+      if (kVec && c + 4 <= n) {
+        if constexpr (kType == GSI_F32) {
+          __stcs(reinterpret_cast<float4*>(static_cast<float*>(to) + at + c), make_float4(x[0], x[1], x[2], x[3]));
+        } else {
+          uint2 v;
+          if constexpr (kType == GSI_BF16) {
+            const __nv_bfloat162 p = __floats2bfloat162_rn(x[0], x[1]), q = __floats2bfloat162_rn(x[2], x[3]);
+            v = make_uint2(*reinterpret_cast<const uint32_t*>(&p), *reinterpret_cast<const uint32_t*>(&q));
+          } else {
+            const __half2 p = __floats2half2_rn(x[0], x[1]), q = __floats2half2_rn(x[2], x[3]);
+            v = make_uint2(*reinterpret_cast<const uint32_t*>(&p), *reinterpret_cast<const uint32_t*>(&q));
+          }
+          __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(to) + at + c), v);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (c + k < n) store_from_float(to, kType, at + c + k, x[k]);
+      }
     }
   }
 }
@@ -366,30 +438,36 @@ int rows_grid(const Shape& s, int n) {
 }  // namespace
 
 cudaError_t launch_plan(const Shape& s, const PlanArgs& a, Control* ctl, cudaStream_t stream) {
-  const long long blocks = ((long long)s.max_tokens + kPlanTokens - 1) / kPlanTokens;
-  k_kv_plan<<<(unsigned)(blocks < kPlanGrid ? blocks : kPlanGrid), kPlanThreads, (size_t)a.n_seqs * 12, stream>>>(s, a, ctl);
-  return cudaGetLastError();
+  const int threads = a.n_seqs <= 128 && s.max_tokens <= 128 * kRun ? 128 : kPlanThreads;
+  const long long blocks = ((long long)s.max_tokens + threads * kRun - 1) / (threads * kRun);
+  return launch_pdl(k_kv_plan, dim3((unsigned)(blocks < kPlanGrid ? blocks : kPlanGrid)), dim3(threads), (size_t)a.n_seqs * 12, stream, s, a, ctl);
 }
 cudaError_t launch_release(const Shape& s, const ReleaseArgs& a, Control* ctl, cudaStream_t stream) {
-  const long long most = (long long)a.n_seqs * s.max_pages, blocks = ((most < s.n_pages ? most : s.n_pages) + kPlanTokens - 1) / kPlanTokens;
-  k_kv_release<<<(unsigned)(blocks < kPlanGrid ? blocks : kPlanGrid), kPlanThreads, (size_t)a.n_seqs * 4, stream>>>(s, a, ctl);
-  return cudaGetLastError();
+  const long long most = (long long)a.n_seqs * s.max_pages, blocks = ((most < s.n_pages ? most : s.n_pages) + kPlanThreads * kRun - 1) / (kPlanThreads * kRun);
+  return launch_pdl(k_kv_release, dim3((unsigned)(blocks < kPlanGrid ? blocks : kPlanGrid)), dim3(kPlanThreads), (size_t)a.n_seqs * 4, stream, s, a, ctl);
+}
+template <gsi_dtype_t kType>
+static cudaError_t append_of(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream) {
+  constexpr long long size = kType == GSI_F32 ? 4 : 2, mask = 4 * size - 1;   // four channels at a time
+  const bool vec = ((reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & mask) == 0 &&
+                   ((a.k_token | a.k_head | a.v_token | a.v_head) * size & mask) == 0;
+  const dim3 grid(rows_grid(s, a.n));
+  return vec ? launch_pdl(k_kv_append<kType, true>, grid, dim3(256), 0, stream, s, a, ctl) : launch_pdl(k_kv_append<kType, false>, grid, dim3(256), 0, stream, s, a, ctl);
+}
+template <gsi_dtype_t kType>
+static cudaError_t read_of(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream) {
+  const uintptr_t mask = kType == GSI_F32 ? 15 : 7;
+  const bool vec = ((reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & mask) == 0 && s.head_dim % 4 == 0;
+  const dim3 grid(rows_grid(s, a.n));
+  return vec ? launch_pdl(k_kv_read<kType, true>, grid, dim3(256), 0, stream, s, a, ctl) : launch_pdl(k_kv_read<kType, false>, grid, dim3(256), 0, stream, s, a, ctl);
 }
 cudaError_t launch_append(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream) {
-  const long long size = a.dtype == GSI_F32 ? 4 : 2;
-  const bool vec = ((reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & 15) == 0 &&
-                   ((a.k_token | a.k_head | a.v_token | a.v_head) * size & 15) == 0;
-  const dim3 grid(rows_grid(s, a.n));
-  if (vec) k_kv_append<true><<<grid, 256, 0, stream>>>(s, a, ctl);
-  else k_kv_append<false><<<grid, 256, 0, stream>>>(s, a, ctl);
-  return cudaGetLastError();
+  return a.dtype == GSI_F32 ? append_of<GSI_F32>(s, a, ctl, stream) : a.dtype == GSI_BF16 ? append_of<GSI_BF16>(s, a, ctl, stream)
+                                                                                        : append_of<GSI_F16>(s, a, ctl, stream);
 }
 cudaError_t launch_read(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream) {
-  const bool vec = ((reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & 15) == 0 && s.head_dim % 4 == 0;
-  const dim3 grid(rows_grid(s, a.n));
-  if (vec) k_kv_read<true><<<grid, 256, 0, stream>>>(s, a, ctl);
-  else k_kv_read<false><<<grid, 256, 0, stream>>>(s, a, ctl);
-  return cudaGetLastError();
+  return a.dtype == GSI_F32 ? read_of<GSI_F32>(s, a, ctl, stream) : a.dtype == GSI_BF16 ? read_of<GSI_BF16>(s, a, ctl, stream)
+                                                                                      : read_of<GSI_F16>(s, a, ctl, stream);
 }
 
 }  // namespace kv

@@ -205,6 +205,8 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
     for (int i = 0; i < C::kBars / 8; ++i) mbar_init(bars + i, N);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   if (tid == 0) s_n_pending = 0;
+  pdl_launch_dependents();
+  pdl_wait();
 
   // ---- shares: the units of all sequences in order, in even pieces that end with a segment where one ends near
   const int per = (a.n_seqs + kScan - 1) / kScan;
@@ -936,8 +938,7 @@ cudaError_t launch(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream
   static_assert(C::kSmem + 6144 <= 232448, "with what else a block holds in shared memory");
   static_assert(C::kRows <= C::kPartRows && 4 * NT <= C::kPartRows && C::kHalf % 16 == 0 && C::kStages >= 1, "layout");
   if (!a.q) return cudaFuncSetAttribute(k_kv_attend<G, T, L, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
-  k_kv_attend<G, T, L, NT><<<kGrid, C::kThreads, C::kSmem, stream>>>(s, a, ctl);
-  return cudaGetLastError();
+  return launch_pdl(k_kv_attend<G, T, L, NT>, dim3(kGrid), dim3(C::kThreads), C::kSmem, stream, s, a, ctl);
 }
 
 // `rows`: of a unit, in column pairs (1, 2, 4, or 8 in two column tiles)
