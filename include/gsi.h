@@ -471,10 +471,11 @@ gsi_status_t gsi_stack_destroy(gsi_stack_t s);
  * ------------------------------------------------------------------------ */
 
 #define GSI_KV_MAX_SEQS 2048
+#define GSI_KV_MAX_HEADS 8192
 #define GSI_KV_MAX_DIM 256
 
 typedef struct {
-  int n_heads;     /* heads of K and V                                              */
+  int n_heads;     /* heads of K and V, 1..GSI_KV_MAX_HEADS                         */
   int head_dim;    /* channels of a head, 1..GSI_KV_MAX_DIM                         */
   int page_tokens; /* a multiple of 16, up to 4096                                  */
   int n_pages;     /* pages of a pool; n_pages * page_tokens < 2^31                 */

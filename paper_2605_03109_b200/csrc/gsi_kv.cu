@@ -3,6 +3,7 @@
 #include <climits>
 #include <cmath>
 #include <new>
+#include <type_traits>
 
 #include "gsi_kv.cuh"
 
@@ -64,7 +65,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
   auto fits = [&](int len, int add) { return add >= 0 && len >= 0 && (long long)len + add <= room; };
   Scan2 sum{0, 0}, total;
   for (int i = first; i < last; ++i) {
-    const int len = a.lens[i], add = __ldg(a.n_new + i);
+    const int len = a.lens[i], add = a.n_new[i];
     sum.a += max(add, 0);
     if (fits(len, add)) sum.b += need_of(len, add);
   }
@@ -74,7 +75,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
     long long row = at.a;
     sum.b = 0;
     for (int i = first; i < last; ++i) {
-      const int len = a.lens[i], add = __ldg(a.n_new + i);
+      const int len = a.lens[i], add = a.n_new[i];
       row += max(add, 0);
       if (fits(len, add) && row <= s.max_tokens) sum.b += need_of(len, add);
     }
@@ -82,7 +83,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
   }
   int took = 0, refused = 0;
   for (int i = first; i < last; ++i) {
-    const int len = a.lens[i], add = __ldg(a.n_new + i);
+    const int len = a.lens[i], add = a.n_new[i];
     s_row[i] = clamp_int(at.a);
     s_page[i] = clamp_int(at.b);
     at.a += max(add, 0);
@@ -137,7 +138,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
       if (len < 0) continue;
       if (left == 0) {
         const int index = p / s.page_tokens, held = pages_of(len, s.page_tokens);
-        const int page = index < held ? a.table[(long long)q * s.max_pages + index] : __ldg(a.free_pages + (n_free - 1 - (s_page[q] + index - held)));
+        const int page = index < held ? a.table[(long long)q * s.max_pages + index] : a.free_pages[n_free - 1 - (s_page[q] + index - held)];
         base = (unsigned)page < (unsigned)s.n_pages ? (page - index) * s.page_tokens : INT_MIN;
         left = (index + 1) * s.page_tokens - p;
         if (base == INT_MIN) ctl->status = GSI_ERR_INVALID_ARG;
@@ -167,12 +168,12 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
   // the new pages
   for (int j = blockIdx.x * threads + threadIdx.x; j < s_took; j += gridDim.x * threads) {
     const int q = last_at_most(s_page, a.n_seqs, j);
-    a.table[(long long)q * s.max_pages + pages_of(s_len[q], s.page_tokens) + j - s_page[q]] = __ldg(a.free_pages + (n_free - 1 - j));
+    a.table[(long long)q * s.max_pages + pages_of(s_len[q], s.page_tokens) + j - s_page[q]] = a.free_pages[n_free - 1 - j];
   }
   if (!a.commit) return;
   if (!read_last(ctl, &s_last)) return;
   for (int i = first; i < last; ++i)
-    if (s_len[i] >= 0) a.lens[i] = s_len[i] + __ldg(a.n_new + i);
+    if (s_len[i] >= 0) a.lens[i] = s_len[i] + a.n_new[i];
   if (threadIdx.x == 0) *a.n_free = n_free - s_took;
 }
 
@@ -221,51 +222,115 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-// Two 16-bit values of a word.
-template <gsi_dtype_t kType>
-__device__ __forceinline__ float2 pair_of(uint32_t w) {
-  if constexpr (kType == GSI_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
-  else return __half22float2(*reinterpret_cast<const __half2*>(&w));
-}
 
-// Channels 4 t + 16 i .. + 3 of a row, i = 0..3, as lane quarter t takes them (four lanes read 64 or 32 bytes in one go); those
-// from n on repeat channel 0 of `at`, which changes neither bound.
-template <gsi_dtype_t kType, bool kVec>
-__device__ __forceinline__ void load_quarters(const void* base, long long at, int t, int n, float (&x)[16]) {
-  if (kVec && n >= kGroup) {
+// Channels 4 t + 16 i .. + 3 of 64, i = 0..3, of a row as they lie in memory: what lane quarter t takes (four lanes read 64
+// or 32 bytes in one go).  Of channels from n on, channel 0 again, which changes neither bound.
+template <gsi_dtype_t kType>
+struct Quarters {
+  static constexpr int kWords = kType == GSI_F32 ? 16 : 8;
+  uint32_t w[kWords];
+
+  template <bool kVec>
+  __device__ __forceinline__ void load(const void* base, long long at, int t, int n) {
+    if (kVec && n >= kGroup) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (kType == GSI_F32) {
-        const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(base) + at) + 4 * i + t);
-        x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
-      } else {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + at) + 4 * i + t);
-        const float2 a = pair_of<kType>(v.x), b = pair_of<kType>(v.y);
-        x[4 * i] = a.x, x[4 * i + 1] = a.y, x[4 * i + 2] = b.x, x[4 * i + 3] = b.y;
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kType == GSI_F32) {
+          const uint4 v = *(reinterpret_cast<const uint4*>(static_cast<const float*>(base) + at) + 4 * i + t);
+          w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+        } else {
+          const uint2 v = *(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + at) + 4 * i + t);
+          w[2 * i] = v.x, w[2 * i + 1] = v.y;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int c = i / 4 * 16 + t * 4 + i % 4;
+        if constexpr (kType == GSI_F32) {
+          w[i] = *(static_cast<const uint32_t*>(base) + at + (c < n ? c : 0));
+        } else {
+          const uint32_t v = *(static_cast<const uint16_t*>(base) + at + (c < n ? c : 0));
+          w[i / 2] = (i & 1) ? w[i / 2] | v << 16 : v;
+        }
       }
     }
-  } else {
+  }
+  __device__ __forceinline__ float channel(int i) const {
+    if constexpr (kType == GSI_F32) return __uint_as_float(w[i]);
+    else if constexpr (kType == GSI_BF16) return __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    else return (i & 1) ? __high2float(*reinterpret_cast<const __half2*>(&w[i / 2])) : __low2float(*reinterpret_cast<const __half2*>(&w[i / 2]));
+  }
+  // NaN where one is.
+  __device__ __forceinline__ void bounds(float* lo, float* hi) const {
+    if constexpr (kType == GSI_F32) {
+      *lo = *hi = channel(0);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int c = i / 4 * 16 + t * 4 + i % 4;
-      x[i] = load_as_float(base, kType, at + (c < n ? c : 0));
+      for (int i = 1; i < 16; ++i) {
+        *lo = min_nan(*lo, channel(i));
+        *hi = max_nan(*hi, channel(i));
+      }
+    } else {
+      using Pair = typename std::conditional<kType == GSI_BF16, __nv_bfloat162, __half2>::type;
+      Pair a = *reinterpret_cast<const Pair*>(&w[0]), b = a;
+#pragma unroll
+      for (int i = 1; i < 8; ++i) {
+        a = __hmin2_nan(a, *reinterpret_cast<const Pair*>(&w[i]));
+        b = __hmax2_nan(b, *reinterpret_cast<const Pair*>(&w[i]));
+      }
+      *lo = min_nan(__low2float(a), __high2float(a));
+      *hi = max_nan(__low2float(b), __high2float(b));
     }
   }
-}
+};
 
-// rint((x - mid) / step) of the four channels c .. c + 3 as signed nibbles.  The quotient, a single fp32 division, is only
-// taken where the product with 1 / step, which is off by 2^-22 of it at most, lies near a border.
-__device__ __forceinline__ uint32_t nibbles4(const float* x, float mid, float step, float inverse) {
-  uint32_t got = 0u;
+// The pair (s, mid) of 64 channels, and what takes their codes.
+struct Scale {
+  __half2 pair;
+  float step, mid, inverse;
+  bool finite, plain;   // plain: no code has to be clamped
+};
+__device__ __forceinline__ Scale scale_of(float lo, float hi) {
+  Scale z;
+  z.finite = lo >= -3.402823466e38f && hi <= 3.402823466e38f;   // (false for NaN)
+  const __half s = __float2half_rn(fminf(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), 65504.f));
+  z.step = __half2float(s);
+  const __half mid = __float2half_rn(fminf(fmaxf(__fadd_rn(lo, 8.f * z.step), -65504.f), 65504.f));
+  z.mid = __half2float(mid);
+  z.inverse = z.step > 0.f ? __fdividef(1.f, z.step) : 0.f;   // (no step: code 8)
+  z.pair = z.finite ? __halves2half2(s, mid) : __half2half2(__ushort_as_half(0x7FFF));
+  z.plain = z.finite && (lo - z.mid) * z.inverse > -8.499f && (hi - z.mid) * z.inverse < 7.499f;
+  return z;
+}
+constexpr float kWhole = 12582912.f;   // 1.5 x 2^23: a sum with it is a whole number of its last digit
+
+// Codes of a lane's sixteen channels, four to 16 bits.  code - 8 = rint((x - mid) / s), where the product with 1 / s serves for
+// the quotient, a single fp32 division: it is off by 8.5 (2^-22 + 2^-24) at most, which only matters next to a border.
+template <gsi_dtype_t kType>
+__device__ __forceinline__ void codes_of(const Quarters<kType>& q, const Scale& z, uint32_t (&got)[4]) {
+  float far = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float d = __fsub_rn(x[i], mid);
-    float r = fminf(fmaxf(d * inverse, -8.f), 7.f);
-    float k = __fadd_rn(r, 12582912.f);   // 1.5 x 2^23: its last bits are the whole number
-    if (fabsf(r - __fsub_rn(k, 12582912.f)) > 0.4999f) k = __fadd_rn(fminf(fmaxf(__fdiv_rn(d, step), -8.f), 7.f), 12582912.f);
-    got |= (__float_as_uint(k) & 15u) << 4 * i;
+    float v = 0.f;
+#pragma unroll
+    for (int k = 3; k >= 0; --k) {
+      const float r = __fsub_rn(q.channel(4 * i + k), z.mid) * z.inverse, whole = __fsub_rn(__fadd_rn(r, kWhole), kWhole);
+      far = fmaxf(far, fabsf(r - whole));
+      v = fmaf(v, 16.f, whole);
+    }
+    got[i] = __float_as_uint(v + (8388608.f + 0x8888)) & 0xFFFFu;   // (the sum of code 16^k, as a whole number)
   }
-  return got;
+  if (z.plain && far < 0.49999f) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    got[i] = 0u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float r = rintf(__fdiv_rn(__fsub_rn(q.channel(4 * i + k), z.mid), z.step));
+      const float code = fminf(fmaxf(__fadd_rn(r, 8.f), 0.f), 15.f);
+      got[i] |= (z.finite ? (uint32_t)code : 0u) << 4 * k;
+    }
+  }
 }
 
 // Of four lanes (quarters t of a row), each with four 16-bit pieces h[i] of piece group i: lane t gets group t's four, in
@@ -281,158 +346,167 @@ __device__ __forceinline__ uint2 transpose4(uint32_t h0, uint32_t h1, uint32_t h
   return make_uint2(__byte_perm(first, second, 0x5410), __byte_perm(first, second, 0x7632));
 }
 
-// A warp takes eight tokens of one head, K or V, 64 channels: four lanes a token, sixteen channels a lane.
+// A warp takes eight tokens of one head, 64 channels of K and of V (of one of them, where rows are few: grid.z = 2): four
+// lanes a token, sixteen channels a lane.  Blocks (head, channels) of the same tokens are neighbours.
+constexpr int kRowWarps = 4;
 struct Item {
-  int row, head, group, is_v;
+  int row, head, group;
 };
-__device__ __forceinline__ Item item_of(const Shape& s, int n, long long w) {
-  Item it;
-  it.group = (int)(w % s.groups);
-  w /= s.groups;
-  it.is_v = (int)(w & 1);
-  w >>= 1;
-  it.head = (int)(w % s.n_heads);
-  it.row = (int)(w / s.n_heads) * 8 + ((threadIdx.x & 31) >> 2);
-  return it;
+__device__ __forceinline__ Item item_of(const Shape& s, long long octet) {
+  const int head = blockIdx.x / s.groups;
+  return {(int)(octet * 8) + (int)(threadIdx.x & 31) / 4, head, (int)blockIdx.x - head * s.groups};
 }
-__host__ __device__ __forceinline__ long long items(const Shape& s, int n) { return ((long long)n + 7) / 8 * s.n_heads * 2 * s.groups; }
+#define FOR_OCTETS(octet, n) \
+  for (long long octet = (long long)blockIdx.y * kRowWarps + (threadIdx.x >> 5); octet * 8 < (n); octet += (long long)gridDim.y * kRowWarps)
 
-// The block of a slot's tile, or null; t: the token within the tile.
+// The block of K of a slot's tile (that of V is as many blocks on as a head has); t: the token within the tile.
 __device__ __forceinline__ unsigned char* block_of(const Shape& s, unsigned char* pages, int slot, const Item& it, int* t) {
   const int page = slot / s.page_tokens, in = slot - page * s.page_tokens;
   *t = in % kTile;
-  return pages + tile_at(s, page, it.head, in / kTile) + (it.is_v * s.groups + it.group) * kBlockBytes;
+  return pages + tile_at(s, page, it.head, in / kTile) + it.group * kBlockBytes;
 }
 
-// Bound by the rows' bytes for long prompts, where 64 channels of a token cost four lanes about 70 instructions each.
+// K and V of a row are under way together.  Bound by issue for long prompts (about 15 instructions a channel and lane), not far above
+// the rows' bytes.
 template <gsi_dtype_t kType, bool kVec>
-__global__ void __launch_bounds__(256) k_kv_append(Shape s, RowsArgs a, Control* ctl) {
+__global__ void __launch_bounds__(kRowWarps * 32) k_kv_append(Shape s, RowsArgs a, Control* ctl) {
   const int quarter = threadIdx.x & 3;
   pdl_launch_dependents();
   pdl_wait();
-  for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < items(s, a.n); w += (long long)gridDim.x * 8) {
-    const Item it = item_of(s, a.n, w);
-    int slot = it.row < a.n ? __ldg(a.slots + it.row) : -1;
+  const int v0 = blockIdx.z, v1 = gridDim.z == 2 ? v0 + 1 : 2;
+  FOR_OCTETS(octet, a.n) {
+    const Item it = item_of(s, octet);
+    int slot = it.row < a.n ? a.slots[it.row] : -1;
     if (slot >= s.n_pages * s.page_tokens) {
       ctl->status = GSI_ERR_INVALID_ARG;
       slot = -1;
     }
-    float x[16];
+    Quarters<kType> rows[2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = 0.f;
-    if (slot >= 0)
-      load_quarters<kType, kVec>(it.is_v ? a.v : a.k, it.row * (it.is_v ? a.v_token : a.k_token) + it.head * (it.is_v ? a.v_head : a.k_head) + it.group * kGroup,
-                                 quarter, s.head_dim - it.group * kGroup, x);
-    float lo = x[0], hi = x[0];
+    for (int v = 0; v < 2; ++v) {
 #pragma unroll
-    for (int i = 1; i < 16; ++i) {
-      lo = min_nan(lo, x[i]);
-      hi = max_nan(hi, x[i]);
+      for (int i = 0; i < Quarters<kType>::kWords; ++i) rows[v].w[i] = 0u;
+      if (slot >= 0 && v >= v0 && v < v1)
+        rows[v].template load<kVec>(v ? a.v : a.k, it.row * (v ? a.v_token : a.k_token) + it.head * (v ? a.v_head : a.k_head) + it.group * kGroup,
+                                    quarter, s.head_dim - it.group * kGroup);
     }
-#pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-      lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-      hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    }
-    const bool finite = lo >= -3.402823466e38f && hi <= 3.402823466e38f;   // (false for NaN)
-    const __half s16 = __float2half_rn(fminf(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), 65504.f));
-    const float step = __half2float(s16);
-    const __half m16 = __float2half_rn(fminf(fmaxf(__fadd_rn(lo, 8.f * step), -65504.f), 65504.f));
-    const float mid = __half2float(m16), inverse = step == 0.f ? 0.f : __fdividef(1.f, step);
-    uint2 code = transpose4(nibbles4(x, mid, step, inverse), nibbles4(x + 4, mid, step, inverse), nibbles4(x + 8, mid, step, inverse),
-                            nibbles4(x + 12, mid, step, inverse), quarter);
-    code.x = step == 0.f ? 0x88888888u : code.x ^ 0x88888888u;   // (8 where there is no step)
-    code.y = step == 0.f ? 0x88888888u : code.y ^ 0x88888888u;
-    if (!finite) code = make_uint2(0u, 0u);
+    const int other = __shfl_xor_sync(0xffffffffu, slot, 4);
     int t = 0;
     unsigned char* block = slot >= 0 ? block_of(s, a.pages, slot, it, &t) : nullptr;
-    // V: a word is four channels of a pair of tokens; where the neighbouring lanes hold the other token of the pair,
-    // each writes one of their two octets of channels whole
-    const int other = __shfl_xor_sync(0xffffffffu, slot, 4);
-    const uint2 far = make_uint2(__shfl_xor_sync(0xffffffffu, code.x, 4), __shfl_xor_sync(0xffffffffu, code.y, 4));
-    if (!block) continue;
-    if (quarter == 0) {
-      const __half2 pair = finite ? __halves2half2(s16, m16) : __half2half2(__ushort_as_half(0x7FFF));
-      *reinterpret_cast<__half2*>(block + pair_byte(t)) = pair;
-    }
-    if (!it.is_v) {
-      *reinterpret_cast<uint2*>(block + k_byte(t, quarter * 16)) = code;
-    } else if (other >= 0 && other == (slot ^ 1)) {
-      const int odd = t & 1;
-      const uint32_t mine = odd ? code.y : code.x, theirs = odd ? far.y : far.x;
-      const uint32_t even_token = odd ? theirs : mine, odd_token = odd ? mine : theirs;
-      *reinterpret_cast<uint2*>(block + v_byte(t & ~1, quarter * 16 + odd * 8)) =
-          make_uint2(__byte_perm(even_token, odd_token, 0x5410), __byte_perm(even_token, odd_token, 0x7632));
-    } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<uint16_t*>(block + v_byte(t, quarter * 16 + i * 4)) = (uint16_t)((i < 2 ? code.x : code.y) >> 16 * (i & 1));
+    for (int v = 0; v < 2; ++v) {
+      if (v < v0 || v >= v1) continue;
+      float lo, hi;
+      rows[v].bounds(&lo, &hi);
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+      }
+      const Scale z = scale_of(lo, hi);
+      uint32_t codes[4];
+      codes_of(rows[v], z, codes);
+      const uint2 code = transpose4(codes[0], codes[1], codes[2], codes[3], quarter);
+      unsigned char* to = block + v * s.groups * kBlockBytes;
+      if (block && quarter == 0) *reinterpret_cast<__half2*>(to + pair_byte(t)) = z.pair;
+      if (!v) {
+        if (block) *reinterpret_cast<uint2*>(to + k_byte(t, quarter * 16)) = code;
+        continue;
+      }
+      // V: a word is four channels of a pair of tokens; where the neighbouring lanes hold the other token of the pair,
+      // each writes one of their two octets of channels whole
+      const uint2 far = make_uint2(__shfl_xor_sync(0xffffffffu, code.x, 4), __shfl_xor_sync(0xffffffffu, code.y, 4));
+      if (!block) continue;
+      if (other >= 0 && other == (slot ^ 1)) {
+        const int odd = t & 1;
+        const uint32_t mine = odd ? code.y : code.x, theirs = odd ? far.y : far.x;
+        const uint32_t even_token = odd ? theirs : mine, odd_token = odd ? mine : theirs;
+        *reinterpret_cast<uint2*>(to + v_byte(t & ~1, quarter * 16 + odd * 8)) =
+            make_uint2(__byte_perm(even_token, odd_token, 0x5410), __byte_perm(even_token, odd_token, 0x7632));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<uint16_t*>(to + v_byte(t, quarter * 16 + i * 4)) = (uint16_t)((i < 2 ? code.x : code.y) >> 16 * (i & 1));
+      }
     }
   }
 }
 
 // A lane quarter takes channels 4 t + 16 i .. + 3, so that four lanes write 64 (32) bytes in one go.
 template <gsi_dtype_t kType, bool kVec>
-__global__ void __launch_bounds__(256) k_kv_read(Shape s, RowsArgs a, Control* ctl) {
+__global__ void __launch_bounds__(kRowWarps * 32) k_kv_read(Shape s, RowsArgs a, Control* ctl) {
   const int quarter = threadIdx.x & 3;
   pdl_launch_dependents();
   pdl_wait();
-  for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < items(s, a.n); w += (long long)gridDim.x * 8) {
-    const Item it = item_of(s, a.n, w);
+  const int v0 = blockIdx.z, v1 = gridDim.z == 2 ? v0 + 1 : 2;
+  FOR_OCTETS(octet, a.n) {
+    const Item it = item_of(s, octet);
     if (it.row >= a.n) continue;
-    int slot = __ldg(a.slots + it.row);
+    int slot = a.slots[it.row];
     if (slot >= s.n_pages * s.page_tokens) {
       ctl->status = GSI_ERR_INVALID_ARG;
       slot = -1;
     }
-    int t = 0;
-    const unsigned char* block = slot >= 0 ? block_of(s, a.pages, slot, it, &t) : nullptr;
-    uint32_t codes[4] = {0u, 0u, 0u, 0u};
-    float2 pair = make_float2(0.f, 0.f);
-    if (block) {
+    uint32_t codes[2][4];
+    __half2 pairs[2];
+    if (slot >= 0) {
+      int t;
+      const unsigned char* block = block_of(s, a.pages, slot, it, &t);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = i * 16 + quarter * 4;
-        codes[i] = *reinterpret_cast<const uint16_t*>(block + (it.is_v ? v_byte(t, c) : k_byte(t, c)));
+      for (int v = 0; v < 2; ++v) {
+        if (v < v0 || v >= v1) continue;
+        const unsigned char* from = block + v * s.groups * kBlockBytes;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c = i * 16 + quarter * 4;
+          codes[v][i] = *reinterpret_cast<const uint16_t*>(from + (v ? v_byte(t, c) : k_byte(t, c)));
+        }
+        pairs[v] = *reinterpret_cast<const __half2*>(from + pair_byte(t));
       }
-      pair = __half22float2(*reinterpret_cast<const __half2*>(block + pair_byte(t)));
     }
-    void* to = it.is_v ? a.v : a.k;
     const long long at = it.row * a.k_token + it.head * a.k_head + it.group * kGroup;
     const int n = s.head_dim - it.group * kGroup;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = i * 16 + quarter * 4;
-      float x[4];
+    for (int v = 0; v < 2; ++v) {
+      if (v < v0 || v >= v1) continue;
+      void* to = v ? a.v : a.k;
+      const float2 pair = __half22float2(pairs[v]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        x[k] = block ? __fmaf_rn(pair.x, (float)((int)(codes[i] >> 4 * k & 15u) - 8), pair.y) : 0.f;   // (the product is exact)
-      if (kVec && c + 4 <= n) {
-        if constexpr (kType == GSI_F32) {
-          __stcs(reinterpret_cast<float4*>(static_cast<float*>(to) + at + c), make_float4(x[0], x[1], x[2], x[3]));
-        } else {
-          uint2 v;
-          if constexpr (kType == GSI_BF16) {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(x[0], x[1]), q = __floats2bfloat162_rn(x[2], x[3]);
-            v = make_uint2(*reinterpret_cast<const uint32_t*>(&p), *reinterpret_cast<const uint32_t*>(&q));
-          } else {
-            const __half2 p = __floats2half2_rn(x[0], x[1]), q = __floats2half2_rn(x[2], x[3]);
-            v = make_uint2(*reinterpret_cast<const uint32_t*>(&p), *reinterpret_cast<const uint32_t*>(&q));
-          }
-          __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(to) + at + c), v);
-        }
-      } else {
+      for (int i = 0; i < 4; ++i) {
+        const int c = i * 16 + quarter * 4;
+        float x[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (c + k < n) store_from_float(to, kType, at + c + k, x[k]);
+          x[k] = slot >= 0 ? __fmaf_rn(pair.x, (float)((int)(codes[v][i] >> 4 * k & 15u) - 8), pair.y) : 0.f;   // (the product is exact)
+        if (kVec && c + 4 <= n) {
+          if constexpr (kType == GSI_F32) {
+            __stcs(reinterpret_cast<float4*>(static_cast<float*>(to) + at + c), make_float4(x[0], x[1], x[2], x[3]));
+          } else {
+            uint2 y;
+            if constexpr (kType == GSI_BF16) {
+              const __nv_bfloat162 p = __floats2bfloat162_rn(x[0], x[1]), q = __floats2bfloat162_rn(x[2], x[3]);
+              y = make_uint2(*reinterpret_cast<const uint32_t*>(&p), *reinterpret_cast<const uint32_t*>(&q));
+            } else {
+              const __half2 p = __floats2half2_rn(x[0], x[1]), q = __floats2half2_rn(x[2], x[3]);
+              y = make_uint2(*reinterpret_cast<const uint32_t*>(&p), *reinterpret_cast<const uint32_t*>(&q));
+            }
+            __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(to) + at + c), y);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (c + k < n) store_from_float(to, kType, at + c + k, x[k]);
+        }
       }
     }
   }
 }
 
-int rows_grid(const Shape& s, int n) {
-  const long long blocks = (items(s, n) + 7) / 8;
-  return (int)(blocks < 148 * 8 ? blocks : 148 * 8);
+dim3 rows_grid(const Shape& s, int n) {
+  const long long wide = (long long)s.n_heads * s.groups, octet_blocks = ((long long)n + 8 * kRowWarps - 1) / (8 * kRowWarps);
+  const long long most = 148 * 16 / wide + 1;   // two rounds of eight blocks an SM
+  // K and V of a row apart, where there are warps for it (64 rows at 16 heads of 256: 7.4 us in and back against 10.5)
+  return dim3((unsigned)wide, (unsigned)(octet_blocks < most ? octet_blocks : most), wide * octet_blocks <= 148 * 4 ? 2 : 1);
 }
 
 }  // namespace
@@ -451,15 +525,15 @@ static cudaError_t append_of(const Shape& s, const RowsArgs& a, Control* ctl, cu
   constexpr long long size = kType == GSI_F32 ? 4 : 2, mask = 4 * size - 1;   // four channels at a time
   const bool vec = ((reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & mask) == 0 &&
                    ((a.k_token | a.k_head | a.v_token | a.v_head) * size & mask) == 0;
-  const dim3 grid(rows_grid(s, a.n));
-  return vec ? launch_pdl(k_kv_append<kType, true>, grid, dim3(256), 0, stream, s, a, ctl) : launch_pdl(k_kv_append<kType, false>, grid, dim3(256), 0, stream, s, a, ctl);
+  const dim3 grid = rows_grid(s, a.n);
+  return vec ? launch_pdl(k_kv_append<kType, true>, grid, dim3(kRowWarps * 32), 0, stream, s, a, ctl) : launch_pdl(k_kv_append<kType, false>, grid, dim3(kRowWarps * 32), 0, stream, s, a, ctl);
 }
 template <gsi_dtype_t kType>
 static cudaError_t read_of(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream) {
   const uintptr_t mask = kType == GSI_F32 ? 15 : 7;
   const bool vec = ((reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & mask) == 0 && s.head_dim % 4 == 0;
-  const dim3 grid(rows_grid(s, a.n));
-  return vec ? launch_pdl(k_kv_read<kType, true>, grid, dim3(256), 0, stream, s, a, ctl) : launch_pdl(k_kv_read<kType, false>, grid, dim3(256), 0, stream, s, a, ctl);
+  const dim3 grid = rows_grid(s, a.n);
+  return vec ? launch_pdl(k_kv_read<kType, true>, grid, dim3(kRowWarps * 32), 0, stream, s, a, ctl) : launch_pdl(k_kv_read<kType, false>, grid, dim3(kRowWarps * 32), 0, stream, s, a, ctl);
 }
 cudaError_t launch_append(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream) {
   return a.dtype == GSI_F32 ? append_of<GSI_F32>(s, a, ctl, stream) : a.dtype == GSI_BF16 ? append_of<GSI_BF16>(s, a, ctl, stream)
@@ -493,7 +567,7 @@ gsi_status_t make_shape(const gsi_kv_desc_t* d, kv::Shape* s) {
   if (!d) return GSI_ERR_INVALID_ARG;
   if (d->n_heads <= 0 || d->head_dim <= 0 || d->page_tokens <= 0 || d->n_pages <= 0 || d->max_seqs <= 0 || d->max_pages <= 0 || d->max_tokens <= 0)
     return GSI_ERR_INVALID_ARG;
-  if (d->head_dim > GSI_KV_MAX_DIM || d->n_heads > 65536 || d->page_tokens % kv::kTile || d->page_tokens > 4096 || d->max_seqs > GSI_KV_MAX_SEQS ||
+  if (d->head_dim > GSI_KV_MAX_DIM || d->n_heads > GSI_KV_MAX_HEADS || d->page_tokens % kv::kTile || d->page_tokens > 4096 || d->max_seqs > GSI_KV_MAX_SEQS ||
       (long long)d->n_pages * d->page_tokens >= 1ll << 31 || (long long)d->max_pages * d->page_tokens > 1ll << 30)
     return GSI_ERR_UNSUPPORTED;
   s->n_heads = d->n_heads;

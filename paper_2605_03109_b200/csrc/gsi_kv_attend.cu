@@ -161,10 +161,10 @@ struct Begin {
 template <int kRows, int kTiles>
 __device__ __forceinline__ Seq load_seq(const Shape& s, const AttendArgs& a, int i) {
   Seq q;
-  q.q0 = __ldg(a.q_start + i);
-  const int end = __ldg(a.q_start + i + 1);
+  q.q0 = a.q_start[i];
+  const int end = a.q_start[i + 1];
   q.m = q.q0 < 0 ? 0 : max(min(end, a.n_rows) - q.q0, 0);
-  q.len = max(__ldg(a.kv_len + i), 0);
+  q.len = max(a.kv_len[i], 0);
   q.seen = q.m ? q.len - (end - q.q0) : 0;
   // (a length outside the table: one tile more than the table has, which is not there)
   const long long room = (long long)s.max_pages * s.page_tiles;
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
       for (int i = 0; i < 2 * G; ++i) {
         const int c = i * 32 + lane;
         v[i] = 0u;
-        if (c < s.head_dim) v[i] = T == 2 ? __ldg(static_cast<const uint32_t*>(a.q) + from + c) : __ldg(static_cast<const uint16_t*>(a.q) + from + c);
+        if (c < s.head_dim) v[i] = T == 2 ? static_cast<const uint32_t*>(a.q)[from + c] : static_cast<const uint16_t*>(a.q)[from + c];
       }
     };
     auto as_float = [&](uint32_t v) {
@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
         const int at = (int)(local - segment * x.units) * N + lane % N, of = (int)quotient(segment, x.n_row_tiles);
         if ((long long)at * kTile < x.len) {
           const int index = at / s.page_tiles;
-          const int page = index < s.max_pages ? __ldg(a.table + (long long)look_seq * s.max_pages + index) : -1;
+          const int page = index < s.max_pages ? a.table[(long long)look_seq * s.max_pages + index] : -1;
           wrong = (unsigned)page >= (unsigned)s.n_pages;
           if (!wrong) where = a.pages + tile_at(s, page, of, at - index * s.page_tiles);
         }
