@@ -14,11 +14,11 @@ namespace {
 
 constexpr int kPlanThreads = 512;
 constexpr int kRun = 8;   // slots of a thread in one round
-constexpr int kPlanGrid = 444;
+constexpr int kPlanGrid = 296;
 
 __device__ __forceinline__ int clamp_int(long long v) { return v > 0x7fffffffll ? 0x7fffffff : (int)v; }
-// (up to 2^31 tokens and a page)
-__device__ __forceinline__ int pages_of(long long tokens, int page_tokens) { return (int)(((unsigned)tokens + page_tokens - 1) / (unsigned)page_tokens); }
+// (up to 2^31 - 4096 tokens)
+__device__ __forceinline__ int pages_of(int tokens, const Shape& s) { return s.by_page.quotient(tokens + s.page_tokens - 1); }
 
 // The last index s with first[s] <= i (first[0] <= i, ascending).
 __device__ __forceinline__ int last_at_most(const int* first, int n, int i) {
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
   const int n_free = min(max(*a.n_free, 0), s.n_pages);
   const int per = (a.n_seqs + threads - 1) / threads, first = threadIdx.x * per, last = min(first + per, a.n_seqs);
   const long long room = (long long)s.max_pages * s.page_tokens;
-  auto need_of = [&](int len, int add) { return pages_of((long long)len + add, s.page_tokens) - pages_of(len, s.page_tokens); };
+  auto need_of = [&](int len, int add) { return pages_of(len + add, s) - pages_of(len, s); };
   auto fits = [&](int len, int add) { return add >= 0 && len >= 0 && (long long)len + add <= room; };
   Scan2 sum{0, 0}, total;
   for (int i = first; i < last; ++i) {
@@ -111,44 +111,51 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
     a.counts[2] = n_free - s_took;
     a.counts[3] = s_refused;
   }
-  // slots and positions, a run of tokens a thread: its sequence is looked up once, a page where it changes
+  // slots and positions, a run of tokens a thread: its sequence and the pages it may touch are looked up once
   const bool vec = ((reinterpret_cast<uintptr_t>(a.slots) | reinterpret_cast<uintptr_t>(a.positions)) & 15) == 0;
+  auto page_of = [&](int q, int len, int index) {   // the page's first slot less its first position; INT_MIN if there is no such page
+    const int held = pages_of(len, s);
+    const int page = index < held ? a.table[(long long)q * s.max_pages + index] : a.free_pages[n_free - 1 - (s_page[q] + index - held)];
+    if ((unsigned)page < (unsigned)s.n_pages) return (page - index) * s.page_tokens;
+    ctl->status = GSI_ERR_INVALID_ARG;
+    return INT_MIN;
+  };
   for (long long i0 = ((long long)blockIdx.x * threads + threadIdx.x) * kRun; i0 < s.max_tokens; i0 += (long long)gridDim.x * threads * kRun) {
     int slot[kRun], pos[kRun];
-    int q = 0, len = -1, p = 0, behind = 0, base = 0, left = 0;   // tokens of the sequence, of the page, that are left
-    if (i0 < n_rows) {
-      q = last_at_most(s_row, a.n_seqs, (int)i0);
-      behind = (q + 1 < a.n_seqs ? s_row[q + 1] : clamp_int(n_rows)) - (int)i0;
-      len = s_len[q];
-      p = len + (int)i0 - s_row[q];
-    }
 #pragma unroll
-    for (int u = 0; u < kRun; ++u) {
-      slot[u] = pos[u] = -1;
-      if (i0 + u >= n_rows) continue;
-      if (behind == 0) {
-        do {
-          ++q;
-          behind = (q + 1 < a.n_seqs ? s_row[q + 1] : clamp_int(n_rows)) - s_row[q];
-        } while (behind == 0);
-        len = p = s_len[q];
-        left = 0;
+    for (int u = 0; u < kRun; ++u) slot[u] = pos[u] = -1;
+    if (i0 < n_rows) {
+      int q = last_at_most(s_row, a.n_seqs, (int)i0);
+      auto behind_of = [&](int x) { return x + 1 < a.n_seqs ? s_row[x + 1] : clamp_int(n_rows); };
+      int behind = behind_of(q) - (int)i0;   // tokens of the sequence that are left
+      if (behind >= kRun) {
+        const int len = s_len[q], p = len + (int)i0 - s_row[q];
+        if (len >= 0) {
+          const int index = s.by_page.quotient(p), left = (index + 1) * s.page_tokens - p;   // (two pages at most)
+          const int base = page_of(q, len, index), next = left < kRun ? page_of(q, len, index + 1) : base;
+#pragma unroll
+          for (int u = 0; u < kRun; ++u) {
+            const int from = u < left ? base : next;
+            pos[u] = from == INT_MIN ? -1 : p + u;
+            slot[u] = from == INT_MIN ? -1 : from + p + u;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < kRun; ++u) {
+          if (i0 + u >= n_rows) continue;
+          while (behind == 0) {
+            ++q;
+            behind = behind_of(q) - s_row[q];
+          }
+          const int len = s_len[q], p = len + (int)(i0 + u) - s_row[q];
+          --behind;
+          if (len < 0) continue;
+          const int from = page_of(q, len, s.by_page.quotient(p));
+          pos[u] = from == INT_MIN ? -1 : p;
+          slot[u] = from == INT_MIN ? -1 : from + p;
+        }
       }
-      --behind;
-      if (len < 0) continue;
-      if (left == 0) {
-        const int index = p / s.page_tokens, held = pages_of(len, s.page_tokens);
-        const int page = index < held ? a.table[(long long)q * s.max_pages + index] : a.free_pages[n_free - 1 - (s_page[q] + index - held)];
-        base = (unsigned)page < (unsigned)s.n_pages ? (page - index) * s.page_tokens : INT_MIN;
-        left = (index + 1) * s.page_tokens - p;
-        if (base == INT_MIN) ctl->status = GSI_ERR_INVALID_ARG;
-      }
-      if (base != INT_MIN) {
-        pos[u] = p;
-        slot[u] = base + p;
-      }
-      ++p;
-      --left;
     }
     if (vec && i0 + kRun <= s.max_tokens) {
 #pragma unroll
@@ -168,7 +175,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
   // the new pages
   for (int j = blockIdx.x * threads + threadIdx.x; j < s_took; j += gridDim.x * threads) {
     const int q = last_at_most(s_page, a.n_seqs, j);
-    a.table[(long long)q * s.max_pages + pages_of(s_len[q], s.page_tokens) + j - s_page[q]] = a.free_pages[n_free - 1 - j];
+    a.table[(long long)q * s.max_pages + pages_of(s_len[q], s) + j - s_page[q]] = a.free_pages[n_free - 1 - j];
   }
   if (!a.commit) return;
   if (!read_last(ctl, &s_last)) return;
@@ -187,7 +194,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_release(Shape s, ReleaseArg
   pdl_wait();
   const int n_free = min(max(*a.n_free, 0), s.n_pages);
   const int per = (a.n_seqs + kPlanThreads - 1) / kPlanThreads, first = threadIdx.x * per, last = min(first + per, a.n_seqs);
-  auto held = [&](int i) { return a.done[i] ? min(pages_of(max(a.lens[i], 0), s.page_tokens), s.max_pages) : 0; };
+  auto held = [&](int i) { return a.done[i] ? min(pages_of(min(max(a.lens[i], 0), 1 << 30), s), s.max_pages) : 0; };
   Scan2 sum{0, 0}, total;
   for (int i = first; i < last; ++i) sum.a += held(i);
   Scan2 at = block_scan(sum, &total, s_warp);
@@ -302,6 +309,16 @@ __device__ __forceinline__ Scale scale_of(float lo, float hi) {
   z.plain = z.finite && (lo - z.mid) * z.inverse > -8.499f && (hi - z.mid) * z.inverse < 7.499f;
   return z;
 }
+__device__ __noinline__ uint32_t exact_codes(float4 x, float mid, float step, bool finite) {
+  uint32_t got = 0u;
+  const float channel[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float code = __fadd_rn(rintf(__fdiv_rn(__fsub_rn(channel[k], mid), step)), 8.f);
+    got |= (uint32_t)fminf(fmaxf(code, 0.f), 15.f) << 4 * k;
+  }
+  return finite ? got : 0u;
+}
 constexpr float kWhole = 12582912.f;   // 1.5 x 2^23: a sum with it is a whole number of its last digit
 
 // Codes of a lane's sixteen channels, four to 16 bits.  code - 8 = rint((x - mid) / s), where the product with 1 / s serves for
@@ -322,15 +339,8 @@ __device__ __forceinline__ void codes_of(const Quarters<kType>& q, const Scale& 
   }
   if (z.plain && far < 0.49999f) return;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    got[i] = 0u;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float r = rintf(__fdiv_rn(__fsub_rn(q.channel(4 * i + k), z.mid), z.step));
-      const float code = fminf(fmaxf(__fadd_rn(r, 8.f), 0.f), 15.f);
-      got[i] |= (z.finite ? (uint32_t)code : 0u) << 4 * k;
-    }
-  }
+  for (int i = 0; i < 4; ++i)
+    got[i] = exact_codes(make_float4(q.channel(4 * i), q.channel(4 * i + 1), q.channel(4 * i + 2), q.channel(4 * i + 3)), z.mid, z.step, z.finite);
 }
 
 // Of four lanes (quarters t of a row), each with four 16-bit pieces h[i] of piece group i: lane t gets group t's four, in
@@ -347,21 +357,20 @@ __device__ __forceinline__ uint2 transpose4(uint32_t h0, uint32_t h1, uint32_t h
 }
 
 // A warp takes eight tokens of one head, 64 channels of K and of V (of one of them, where rows are few: grid.z = 2): four
-// lanes a token, sixteen channels a lane.  Blocks (head, channels) of the same tokens are neighbours.
+// lanes a token, sixteen channels a lane.  Blocks of the same tokens are neighbours: heads, or (head, channels) where rows are few.
 constexpr int kRowWarps = 4;
 struct Item {
   int row, head, group;
 };
-__device__ __forceinline__ Item item_of(const Shape& s, long long octet) {
-  const int head = blockIdx.x / s.groups;
-  return {(int)(octet * 8) + (int)(threadIdx.x & 31) / 4, head, (int)blockIdx.x - head * s.groups};
+__device__ __forceinline__ Item item_of(const Shape& s, long long octet, int head, int group) {
+  return {(int)(octet * 8) + (int)(threadIdx.x & 31) / 4, head, group};
 }
 #define FOR_OCTETS(octet, n) \
   for (long long octet = (long long)blockIdx.y * kRowWarps + (threadIdx.x >> 5); octet * 8 < (n); octet += (long long)gridDim.y * kRowWarps)
 
 // The block of K of a slot's tile (that of V is as many blocks on as a head has); t: the token within the tile.
 __device__ __forceinline__ unsigned char* block_of(const Shape& s, unsigned char* pages, int slot, const Item& it, int* t) {
-  const int page = slot / s.page_tokens, in = slot - page * s.page_tokens;
+  const int page = s.by_page.quotient(slot), in = slot - page * s.page_tokens;
   *t = in % kTile;
   return pages + tile_at(s, page, it.head, in / kTile) + it.group * kBlockBytes;
 }
@@ -369,30 +378,30 @@ __device__ __forceinline__ unsigned char* block_of(const Shape& s, unsigned char
 // K and V of a row are under way together.  Bound by issue for long prompts (about 15 instructions a channel and lane), not far above
 // the rows' bytes.
 template <gsi_dtype_t kType, bool kVec>
-__global__ void __launch_bounds__(kRowWarps * 32) k_kv_append(Shape s, RowsArgs a, Control* ctl) {
+__global__ void __launch_bounds__(kRowWarps * 32, kType == GSI_F32 ? 7 : 8) k_kv_append(Shape s, RowsArgs a, Control* ctl) {
   const int quarter = threadIdx.x & 3;
   pdl_launch_dependents();
   pdl_wait();
   const int v0 = blockIdx.z, v1 = gridDim.z == 2 ? v0 + 1 : 2;
+  const bool whole = gridDim.x == s.n_heads;   // all channels of a head
+  const int head = whole ? blockIdx.x : blockIdx.x / s.groups, g0 = whole ? 0 : blockIdx.x - head * s.groups, g1 = whole ? s.groups : g0 + 1;
   FOR_OCTETS(octet, a.n) {
-    const Item it = item_of(s, octet);
+    Item it = item_of(s, octet, head, g0);
     int slot = it.row < a.n ? a.slots[it.row] : -1;
     if (slot >= s.n_pages * s.page_tokens) {
       ctl->status = GSI_ERR_INVALID_ARG;
       slot = -1;
     }
-    Quarters<kType> rows[2];
-#pragma unroll
-    for (int v = 0; v < 2; ++v) {
-#pragma unroll
-      for (int i = 0; i < Quarters<kType>::kWords; ++i) rows[v].w[i] = 0u;
-      if (slot >= 0 && v >= v0 && v < v1)
-        rows[v].template load<kVec>(v ? a.v : a.k, it.row * (v ? a.v_token : a.k_token) + it.head * (v ? a.v_head : a.k_head) + it.group * kGroup,
-                                    quarter, s.head_dim - it.group * kGroup);
-    }
+    const int from = min(it.row, a.n - 1);   // (a row that goes nowhere is read all the same)
     const int other = __shfl_xor_sync(0xffffffffu, slot, 4);
     int t = 0;
-    unsigned char* block = slot >= 0 ? block_of(s, a.pages, slot, it, &t) : nullptr;
+    unsigned char* first = slot >= 0 ? block_of(s, a.pages, slot, it, &t) : nullptr;
+    const long long k_at = from * a.k_token + head * a.k_head, v_at = from * a.v_token + head * a.v_head;
+    for (; it.group < g1; ++it.group) {
+    Quarters<kType> rows[2];
+    if (v0 == 0) rows[0].template load<kVec>(a.k, k_at + it.group * kGroup, quarter, s.head_dim - it.group * kGroup);
+    if (v1 == 2) rows[1].template load<kVec>(a.v, v_at + it.group * kGroup, quarter, s.head_dim - it.group * kGroup);
+    unsigned char* block = first + (it.group - g0) * kBlockBytes;
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
       if (v < v0 || v >= v1) continue;
@@ -408,15 +417,15 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_kv_append(Shape s, RowsArgs 
       codes_of(rows[v], z, codes);
       const uint2 code = transpose4(codes[0], codes[1], codes[2], codes[3], quarter);
       unsigned char* to = block + v * s.groups * kBlockBytes;
-      if (block && quarter == 0) *reinterpret_cast<__half2*>(to + pair_byte(t)) = z.pair;
+      if (first && quarter == 0) *reinterpret_cast<__half2*>(to + pair_byte(t)) = z.pair;
       if (!v) {
-        if (block) *reinterpret_cast<uint2*>(to + k_byte(t, quarter * 16)) = code;
+        if (first) *reinterpret_cast<uint2*>(to + k_byte(t, quarter * 16)) = code;
         continue;
       }
       // V: a word is four channels of a pair of tokens; where the neighbouring lanes hold the other token of the pair,
       // each writes one of their two octets of channels whole
       const uint2 far = make_uint2(__shfl_xor_sync(0xffffffffu, code.x, 4), __shfl_xor_sync(0xffffffffu, code.y, 4));
-      if (!block) continue;
+      if (!first) continue;
       if (other >= 0 && other == (slot ^ 1)) {
         const int odd = t & 1;
         const uint32_t mine = odd ? code.y : code.x, theirs = odd ? far.y : far.x;
@@ -429,6 +438,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_kv_append(Shape s, RowsArgs 
           *reinterpret_cast<uint16_t*>(to + v_byte(t, quarter * 16 + i * 4)) = (uint16_t)((i < 2 ? code.x : code.y) >> 16 * (i & 1));
       }
     }
+    }
   }
 }
 
@@ -439,8 +449,9 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_kv_read(Shape s, RowsArgs a,
   pdl_launch_dependents();
   pdl_wait();
   const int v0 = blockIdx.z, v1 = gridDim.z == 2 ? v0 + 1 : 2;
+  const int head = blockIdx.x / s.groups, group = blockIdx.x - head * s.groups;
   FOR_OCTETS(octet, a.n) {
-    const Item it = item_of(s, octet);
+    const Item it = item_of(s, octet, head, group);
     if (it.row >= a.n) continue;
     int slot = a.slots[it.row];
     if (slot >= s.n_pages * s.page_tokens) {
@@ -502,11 +513,13 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_kv_read(Shape s, RowsArgs a,
   }
 }
 
-dim3 rows_grid(const Shape& s, int n) {
-  const long long wide = (long long)s.n_heads * s.groups, octet_blocks = ((long long)n + 8 * kRowWarps - 1) / (8 * kRowWarps);
-  const long long most = 148 * 16 / wide + 1;   // two rounds of eight blocks an SM
-  // K and V of a row apart, where there are warps for it (64 rows at 16 heads of 256: 7.4 us in and back against 10.5)
-  return dim3((unsigned)wide, (unsigned)(octet_blocks < most ? octet_blocks : most), wide * octet_blocks <= 148 * 4 ? 2 : 1);
+dim3 rows_grid(const Shape& s, int n, bool whole_heads) {
+  const long long octet_blocks = ((long long)n + 8 * kRowWarps - 1) / (8 * kRowWarps);
+  // K and V of a row, and the blocks of a head, apart where there are warps for it (64 rows at 16 heads of 256: 7.3 us in and
+  // back against 10.5)
+  const bool few = (long long)s.n_heads * s.groups * octet_blocks <= 148 * 4;
+  const long long wide = few || !whole_heads ? (long long)s.n_heads * s.groups : s.n_heads, most = 65535;
+  return dim3((unsigned)wide, (unsigned)(octet_blocks < most ? octet_blocks : most), few ? 2 : 1);
 }
 
 }  // namespace
@@ -525,14 +538,14 @@ static cudaError_t append_of(const Shape& s, const RowsArgs& a, Control* ctl, cu
   constexpr long long size = kType == GSI_F32 ? 4 : 2, mask = 4 * size - 1;   // four channels at a time
   const bool vec = ((reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & mask) == 0 &&
                    ((a.k_token | a.k_head | a.v_token | a.v_head) * size & mask) == 0;
-  const dim3 grid = rows_grid(s, a.n);
+  const dim3 grid = rows_grid(s, a.n, true);
   return vec ? launch_pdl(k_kv_append<kType, true>, grid, dim3(kRowWarps * 32), 0, stream, s, a, ctl) : launch_pdl(k_kv_append<kType, false>, grid, dim3(kRowWarps * 32), 0, stream, s, a, ctl);
 }
 template <gsi_dtype_t kType>
 static cudaError_t read_of(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream) {
   const uintptr_t mask = kType == GSI_F32 ? 15 : 7;
   const bool vec = ((reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & mask) == 0 && s.head_dim % 4 == 0;
-  const dim3 grid = rows_grid(s, a.n);
+  const dim3 grid = rows_grid(s, a.n, false);
   return vec ? launch_pdl(k_kv_read<kType, true>, grid, dim3(kRowWarps * 32), 0, stream, s, a, ctl) : launch_pdl(k_kv_read<kType, false>, grid, dim3(kRowWarps * 32), 0, stream, s, a, ctl);
 }
 cudaError_t launch_append(const Shape& s, const RowsArgs& a, Control* ctl, cudaStream_t stream) {
@@ -579,6 +592,8 @@ gsi_status_t make_shape(const gsi_kv_desc_t* d, kv::Shape* s) {
   s->max_seqs = d->max_seqs;
   s->max_pages = d->max_pages;
   s->max_tokens = d->max_tokens;
+  s->by_page = kv::Divisor::of(s->page_tokens);
+  s->by_page_tiles = kv::Divisor::of(s->page_tiles);
   s->tile_bytes = 2ll * s->groups * kv::kBlockBytes;
   s->head_bytes = s->page_tiles * s->tile_bytes;
   s->page_bytes = s->n_heads * s->head_bytes;

@@ -28,8 +28,21 @@ __host__ __device__ __forceinline__ int v_byte(int t, int c) {
 }
 __host__ __device__ __forceinline__ int pair_byte(int t) { return kCodeBytes + (2 * (t % 8) + t / 8) * 4; }
 
+// n / d for 0 <= n < 2^31: n m / 2^(31 + l) with 2^(l - 1) < d <= 2^l and m = ceil(2^(31 + l) / d), which is less than 2^32
+// and off by less than 2^l / 2^31 of a unit of the quotient.
+struct Divisor {
+  unsigned d, mul, shift;
+  static Divisor of(int d) {
+    unsigned l = 0;
+    while ((1ull << l) < (unsigned long long)d) ++l;
+    return {(unsigned)d, (unsigned)(((1ull << (31 + l)) + d - 1) / d), 31 + l};
+  }
+  __host__ __device__ __forceinline__ int quotient(int n) const { return (int)((unsigned long long)(unsigned)n * mul >> shift); }
+};
+
 struct Shape {
   int n_heads, head_dim, groups, page_tokens, page_tiles, n_pages, max_seqs, max_pages, max_tokens;
+  Divisor by_page, by_page_tiles;                 // of tokens, of tiles
   long long tile_bytes, head_bytes, page_bytes;   // a tile of a head (K and V), a head of a page, a page
 };
 

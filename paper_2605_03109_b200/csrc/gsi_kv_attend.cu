@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
         const long long local = u - look_base, segment = quotient(local, x.units);
         const int at = (int)(local - segment * x.units) * N + lane % N, of = (int)quotient(segment, x.n_row_tiles);
         if ((long long)at * kTile < x.len) {
-          const int index = at / s.page_tiles;
+          const int index = s.by_page_tiles.quotient(at);
           const int page = index < s.max_pages ? a.table[(long long)look_seq * s.max_pages + index] : -1;
           wrong = (unsigned)page >= (unsigned)s.n_pages;
           if (!wrong) where = a.pages + tile_at(s, page, of, at - index * s.page_tiles);
