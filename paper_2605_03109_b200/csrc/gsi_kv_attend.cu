@@ -67,7 +67,7 @@ struct Cfg {
   static constexpr int kWarpBytes = (kRing + kQ + kSums + kBars + 15) / 16 * 16;
   static constexpr int kSmem = kWarps * kWarpBytes;
   static_assert(kShares <= kMaxShares, "the workspace's parts and tickets");
-  static constexpr int kSnap = kTiles == 1 ? 4 : 2;    // units: the share of a warp ends with a segment that ends as near
+  static constexpr int kSnap = kTiles == 1 ? 2 : 1;    // units: the share of a warp ends with a segment that ends as near
   static constexpr int kCost = L + 1;                    // units that a segment itself counts as in a share
   static constexpr int kPart = kPartFloats(G);
   static constexpr int kPartRows = kPart / (kDim + 8);
