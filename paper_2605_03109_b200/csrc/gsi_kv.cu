@@ -13,7 +13,7 @@ namespace kv {
 namespace {
 
 constexpr int kPlanThreads = 512;
-constexpr int kRun = 8;   // slots of a thread in one round
+constexpr int kLongRun = 8;   // slots of a thread in one round, where they are many
 constexpr int kPlanGrid = 296;
 
 __device__ __forceinline__ int clamp_int(long long v) { return v > 0x7fffffffll ? 0x7fffffff : (int)v; }
@@ -47,6 +47,7 @@ __device__ __forceinline__ bool read_last(Control* ctl, int* s_last) {
 // another; the sequences' first rows and first pages stay in shared memory, where each run of tokens and each page of the
 // block looks up its own.  The block that is last to have read the state moves it on.
 // Bound by the launch and three dependent reads (one token: 4.1 us a call); for prompts by the writes of slots and positions.
+template <int kRun>
 __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, Control* ctl) {
   extern __shared__ int sm[];
   int* s_row = sm;                    // first row of a sequence
@@ -157,9 +158,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
         }
       }
     }
-    if (vec && i0 + kRun <= s.max_tokens) {
+    if (kRun % 4 == 0 && vec && i0 + kRun <= s.max_tokens) {
 #pragma unroll
-      for (int u = 0; u < kRun; u += 4) {
+      for (int u = 0; u + 3 < kRun; u += 4) {
         *reinterpret_cast<int4*>(a.slots + i0 + u) = make_int4(slot[u], slot[u + 1], slot[u + 2], slot[u + 3]);
         *reinterpret_cast<int4*>(a.positions + i0 + u) = make_int4(pos[u], pos[u + 1], pos[u + 2], pos[u + 3]);
       }
@@ -525,12 +526,15 @@ dim3 rows_grid(const Shape& s, int n, bool whole_heads) {
 }  // namespace
 
 cudaError_t launch_plan(const Shape& s, const PlanArgs& a, Control* ctl, cudaStream_t stream) {
-  const int threads = a.n_seqs <= 128 && s.max_tokens <= 128 * kRun ? 128 : kPlanThreads;
-  const long long blocks = ((long long)s.max_tokens + threads * kRun - 1) / (threads * kRun);
-  return launch_pdl(k_kv_plan, dim3((unsigned)(blocks < kPlanGrid ? blocks : kPlanGrid)), dim3(threads), (size_t)a.n_seqs * 12, stream, s, a, ctl);
+  // A token a thread for decode steps (64 requests: 3.3 us a call against 5.2), runs of them for prompts.
+  const bool one = s.max_tokens <= kPlanThreads * 4;
+  const int threads = a.n_seqs <= 128 && s.max_tokens <= 128 ? 128 : kPlanThreads, run = one ? 1 : kLongRun;
+  const long long blocks = ((long long)s.max_tokens + threads * run - 1) / (threads * run);
+  return launch_pdl(one ? k_kv_plan<1> : k_kv_plan<kLongRun>, dim3((unsigned)(blocks < kPlanGrid ? blocks : kPlanGrid)), dim3(threads), (size_t)a.n_seqs * 12,
+                    stream, s, a, ctl);
 }
 cudaError_t launch_release(const Shape& s, const ReleaseArgs& a, Control* ctl, cudaStream_t stream) {
-  const long long most = (long long)a.n_seqs * s.max_pages, blocks = ((most < s.n_pages ? most : s.n_pages) + kPlanThreads * kRun - 1) / (kPlanThreads * kRun);
+  const long long most = (long long)a.n_seqs * s.max_pages, blocks = ((most < s.n_pages ? most : s.n_pages) + kPlanThreads * kLongRun - 1) / (kPlanThreads * kLongRun);
   return launch_pdl(k_kv_release, dim3((unsigned)(blocks < kPlanGrid ? blocks : kPlanGrid)), dim3(kPlanThreads), (size_t)a.n_seqs * 4, stream, s, a, ctl);
 }
 template <gsi_dtype_t kType>

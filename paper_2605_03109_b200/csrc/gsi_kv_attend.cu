@@ -559,14 +559,14 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int r = 0; r < kLR; ++r) {
-            if constexpr (kMasked) {
+            if constexpr (kMasked) {   // (scaled here: a factor of 0, or below, would make something else of infinity)
               const int vis = sees(row_of(n, r)) - pos;
-              S[n][r][0] = vis <= 0 ? -INFINITY : wrong ? NAN : S[n][r][0];
-              S[n][r][1] = vis <= 8 ? -INFINITY : wrong ? NAN : S[n][r][1];
+              S[n][r][0] = vis <= 0 ? -INFINITY : wrong ? NAN : S[n][r][0] * factor[n][r];
+              S[n][r][1] = vis <= 8 ? -INFINITY : wrong ? NAN : S[n][r][1] * factor[n][r];
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              p[n][r][e] = fmaf(S[n][r][e], factor[n][r], -m[n][r]);
+              p[n][r][e] = fmaf(S[n][r][e], kMasked ? 1.f : factor[n][r], -m[n][r]);
               move = move || p[n][r][e] > kLazy;
             }
           }
@@ -583,7 +583,8 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < kLR; ++r) {
-              float x = fmaxf(m[n][r], fmaxf(S[n][r][0] * factor[n][r], S[n][r][1] * factor[n][r]));
+              const float f = kMasked ? 1.f : factor[n][r];
+              float x = fmaxf(m[n][r], fmaxf(S[n][r][0] * f, S[n][r][1] * f));
 #pragma unroll
               for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
               if (x - m[n][r] <= kLazy) x = m[n][r];   // (another row's: this one's sums stay as they are)
@@ -594,7 +595,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
               for (int g = 0; g < G; ++g) z[n][r][g] *= keep[n][r];
               keep[n][r] *= v_keep;
 #pragma unroll
-              for (int e = 0; e < 2; ++e) p[n][r][e] = fmaf(S[n][r][e], factor[n][r], -x);
+              for (int e = 0; e < 2; ++e) p[n][r][e] = fmaf(S[n][r][e], f, -x);
             }
 #pragma unroll
           for (int n = 0; n < NT; ++n)

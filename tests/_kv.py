@@ -54,25 +54,19 @@ def block(desc, slot, head, group, is_v):
     return (((page * n_heads + head) * tiles + tile) * 2 + is_v) * G * 576 + group * 576
 
 
-def decode(pool, desc, slots):
-    """(codes, s, mid) of K and of V, [n][heads][...], of the tokens in `slots`; pool: bytes."""
+def decode(pool, desc, slots, heads=None):
+    """(codes, s, mid) of K and of V, [n][heads][...], of the tokens in `slots`; pool: bytes; heads: all, or some of them."""
     n_heads, dim, _ = desc
     G = -(-dim // 64)
+    slots = np.asarray(slots, np.int64).reshape(-1, 1, 1)
+    h = np.arange(n_heads) if heads is None else np.asarray(heads)
+    h, c, g, t = h.reshape(1, -1, 1), np.arange(dim), np.arange(G), slots % 16
     got = []
     for is_v in (0, 1):
-        codes = np.zeros((len(slots), n_heads, dim), np.uint8)
-        pairs = np.zeros((2, len(slots), n_heads, G), np.float16)
-        c = np.arange(dim)
-        for i, slot in enumerate(slots):
-            t = slot % 16
-            inside = np.array([(v_byte if is_v else k_byte)(t, x) for x in c % 64]) + c // 64 * 576
-            for h in range(n_heads):
-                at = block(desc, slot, h, 0, is_v)
-                codes[i, h] = pool[at + inside] >> (4 * (c % 2)) & 15
-                for g in range(G):
-                    p = at + 576 * g + pair_byte(t)
-                    pairs[:, i, h, g] = pool[p:p + 4].view(np.float16)
-        got.append((codes, pairs[0], pairs[1]))
+        at = block(desc, slots, h, 0, is_v)
+        codes = pool[at + c // 64 * 576 + (v_byte if is_v else k_byte)(t, c % 64)] >> (4 * (c % 2)).astype(np.uint8) & 15
+        pairs = np.ascontiguousarray(pool[(at + 576 * g + pair_byte(t))[..., None] + np.arange(4)]).view(np.float16)
+        got.append((codes, pairs[..., 0], pairs[..., 1]))
     return got
 
 

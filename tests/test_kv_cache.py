@@ -305,16 +305,25 @@ def test_a_plan_for_empty_requests_and_their_release_leave_the_pool_as_it_was():
         assert torch.equal(c.free, free) and c.n_free.item() == 4000 and not c.lens.any() and (c.table == -1).all()
 
 
+def slots_of(c, kv_len, table):
+    got = [table[i, np.arange(n) // c.page_tokens] * c.page_tokens + np.arange(n) % c.page_tokens for i, n in enumerate(kv_len)]
+    return np.concatenate(got).astype(np.int32)
+
+
 def fill(c, rng, kv_len, table):
     """Random tokens of the lengths `kv_len`; everything else of the pool is what makes a kernel that reads it wrong."""
     c.pages.fill_(0xFF)      # (all codes 15, all pairs NaN)
-    slots = np.concatenate([[table[i, p // c.page_tokens] * c.page_tokens + p % c.page_tokens for p in range(n)] for i, n in enumerate(kv_len)] + [[]])
-    slots = slots.astype(np.int32)
+    slots = slots_of(c, kv_len, table)
     if len(slots):
-        k, v = (torch.from_numpy((rng.standard_normal((len(slots), c.n_heads, c.head_dim)) * s).astype(np.float32)).cuda() for s in (1.5, 1.0))
+        g = torch.Generator("cuda").manual_seed(int(rng.integers(1 << 30)))
+        k, v = (torch.randn(len(slots), c.n_heads, c.head_dim, device="cuda", generator=g) * s for s in (1.5, 1.0))
         k[:, :, 0] *= 5
-        c.append(k, v + 0.1, slots=ints(slots.tolist()))
-    return read_back(c, slots)
+        c.append(k, v + 0.1, slots=torch.from_numpy(slots).cuda())
+    return slots
+
+
+def fill_and_read(c, rng, kv_len, table):
+    return read_back(c, fill(c, rng, kv_len, table))
 
 
 def check(c, q, out, before, kv, kv_len, news, scale):
@@ -324,7 +333,6 @@ def check(c, q, out, before, kv, kv_len, news, scale):
     shared = q.shape[1] // c.n_heads
     qn, got = q.float().cpu().numpy(), out.double().cpu().numpy()
     row = first = 0
-    worst = 0.0
     for n, m in zip(kv_len, news):
         part = [[x[first:first + n] for x in t] for t in kv]
         for i in range(m):
@@ -337,11 +345,9 @@ def check(c, q, out, before, kv, kv_len, news, scale):
                 want, off = R.attend(qn[row, h], *have, scale, sixteen)
                 tol = off + half * np.abs(want) + (6e-8 if out.dtype == torch.float16 else 0)   # (f16's smallest step)
                 assert (np.abs(got[row, h] - want) <= tol).all(), (row, h, sees, float((np.abs(got[row, h] - want) / tol).max()))
-                worst = max(worst, float((np.abs(got[row, h] - want) / tol).max()))
             row += 1
         first += n
     assert torch.equal(out[row:], before[row:])
-    return worst
 
 
 def a_cache(heads, dim, page, kv_len, news, rng, extra=2):
@@ -376,7 +382,7 @@ LENGTHS = [
 def test_attention_is_the_one_in_64_bits(dtype, name, kv_len, news, heads, shared, dim, page):
     rng = np.random.default_rng(len(name) + dim)
     c, table = a_cache(heads, dim, page, kv_len, news, rng)
-    kv = fill(c, rng, kv_len, table)
+    kv = fill_and_read(c, rng, kv_len, table)
     n = sum(news)
     q = rows(rng, (n + 2, heads * shared, dim), dtype, 1.3)
     out = torch.full_like(q, 9.0)
@@ -394,7 +400,7 @@ def test_rows_of_any_stride(dtype):
     rng = np.random.default_rng(3)
     kv_len, news = [37, 5], [3, 1]
     c, table = a_cache(2, 64, 16, kv_len, news, rng)
-    kv = fill(c, rng, kv_len, table)
+    kv = fill_and_read(c, rng, kv_len, table)
     wide = rows(rng, (4, 3 + 5 * 64), dtype)
     q = wide[:, 3:3 + 4 * 64].unflatten(1, (4, 64))                     # rows that begin nowhere in particular
     turned = rows(rng, (4, 4, 64), dtype).transpose(0, 1)               # heads outside, tokens inside
@@ -411,7 +417,7 @@ def test_rows_of_any_stride(dtype):
 def test_q_of_any_size(size):
     rng = np.random.default_rng(4)
     c, table = a_cache(1, 128, 16, [45], [1], rng)
-    kv = fill(c, rng, [45], table)
+    kv = fill_and_read(c, rng, [45], table)
     q = rows(rng, (1, 2, 128), torch.float32)
     q = (q.double() * size).float()
     q[:, 1, ::3] = 0.0
@@ -444,7 +450,7 @@ def test_what_is_not_a_number_stays_where_it_is_seen():
     kv_len, news = [60, 40], [20, 1]
     for dtype in (torch.float32, torch.float16):
         c, table = a_cache(2, 128, 16, kv_len, news, rng)
-        kv = fill(c, rng, kv_len, table)
+        kv = fill_and_read(c, rng, kv_len, table)
         q = rows(rng, (21, 2, 128), dtype)
         clean = c.attend(q)
         check(c, q, clean, clean, kv, kv_len, news, 128 ** -0.5)
@@ -470,7 +476,7 @@ def test_pages_and_lengths_outside_are_reported():
     kv_len, news = [40, 40, 40], [1, 2, 1]
     for bad in (-1, 1 << 30, 99):
         c, table = a_cache(1, 64, 16, kv_len, news, rng)
-        kv = fill(c, rng, kv_len, table)
+        kv = fill_and_read(c, rng, kv_len, table)
         q = rows(rng, (4, 1, 64), torch.float32)
         clean = c.attend(q)
         assert c.status() == 0
@@ -496,13 +502,110 @@ def test_requests_over_the_whole_grid():
     for heads, dim, kv_len in ((1, 64, [int(x) for x in rng.integers(0, 40, 900)]), (1, 128, [6000]), (2, 64, [2000] + [3] * 100 + [0] * 30 + [1500])):
         news = [1] * len(kv_len)
         c, table = a_cache(heads, dim, 64, kv_len, news, rng)
-        kv = fill(c, rng, kv_len, table)
+        kv = fill_and_read(c, rng, kv_len, table)
         for dtype in (torch.float32, torch.bfloat16):
             q = rows(rng, (len(news), heads, dim), dtype)
             out = c.attend(q)
             check(c, q, out, out, kv, kv_len, news, dim ** -0.5)
             for _ in range(3):
                 assert torch.equal(c.attend(q), out)
+
+
+def check_some(c, q, out, kv_len, news, slots, scale, which):
+    """check() of the rows of some (request, head of the cache)."""
+    pool = c.pages.view(-1).cpu().numpy()
+    first, row = np.concatenate([[0], np.cumsum(kv_len)]), np.concatenate([[0], np.cumsum(news)])
+    shared, sixteen, half = q.shape[1] // c.n_heads, out.dtype != torch.float32, torch.finfo(out.dtype).eps / 2
+    qn, got = q.float().cpu().numpy(), out.double().cpu().numpy()
+    for i, h in which:
+        k, v = R.decode(pool, (c.n_heads, c.head_dim, c.page_tokens), slots[first[i]:first[i + 1]], [h])
+        for m in sorted({0, news[i] // 2, news[i] - 1}):
+            sees = kv_len[i] - news[i] + m + 1
+            for x in sorted({h * shared, h * shared + shared - 1}):
+                want, off = R.attend(qn[row[i] + m, x], *[[y[:sees, 0] for y in z] for z in (k, v)], scale, sixteen)
+                tol = off + half * np.abs(want)
+                assert (np.abs(got[row[i] + m, x] - want) <= tol).all(), (i, h, m, x)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+@pytest.mark.parametrize("shared,new", [(1, 1), (2, 1), (1, 3), (5, 1), (2, 9)])
+def test_one_long_request_over_the_whole_grid(dtype, dim, shared, new):
+    """Sums of hundreds of warps meet: of one row and of many."""
+    rng = np.random.default_rng(dim + shared)
+    kv_len, news = [20011], [new]
+    c, table = a_cache(1, dim, 48, kv_len, news, rng)
+    slots = fill(c, rng, kv_len, table)
+    q = rows(rng, (new, shared, dim), dtype)
+    out = c.attend(q)
+    check_some(c, q, out, kv_len, news, slots, dim ** -0.5, [(0, 0)])
+    assert torch.equal(c.attend(q), out) and c.status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("seqs,heads,length,new", [(8, 64, 10007, 1), (8, 32, 5009, 4), (4, 16, 20011, 2)])
+def test_long_shares(dtype, seqs, heads, length, new):
+    """Every warp has more tokens than the tensor cores sum at a time."""
+    rng = np.random.default_rng(seqs)
+    kv_len, news = [length - 13 * i for i in range(seqs)], [new] * seqs
+    c, table = a_cache(heads, 64, 64, kv_len, news, rng)
+    slots = fill(c, rng, kv_len, table)
+    q = rows(rng, (sum(news), heads, 64), dtype)
+    out = c.attend(q)
+    which = [(0, 0), (seqs - 1, heads - 1)] + [(int(rng.integers(seqs)), int(rng.integers(heads))) for _ in range(6)]
+    check_some(c, q, out, kv_len, news, slots, 0.125, which)
+    assert torch.equal(c.attend(q), out)
+
+
+@gpu
+@pytest.mark.parametrize("dim", [1, 3, 8, 65, 129, 193, 255])
+def test_heads_of_any_width(dim):
+    rng = np.random.default_rng(dim)
+    kv_len, news = [70, 3, 18], [1, 1, 2]
+    c, table = a_cache(2, dim, 16, kv_len, news, rng)
+    kv = fill_and_read(c, rng, kv_len, table)
+    for dtype in DTYPES:
+        q = rows(rng, (4, 4, dim), dtype)
+        out = torch.full((4, 4, dim + 1), 9.0, dtype=dtype, device="cuda")
+        c.attend(q, out=out[:, :, :dim])
+        check(c, q, out[:, :, :dim], out[:, :, :dim], kv, kv_len, news, dim ** -0.5)
+        assert (out[:, :, dim] == 9).all()
+
+
+@gpu
+def test_many_q_heads_and_scales_of_any_sign():
+    rng = np.random.default_rng(12)
+    kv_len, news = [33, 100], [1, 3]
+    c, table = a_cache(1, 64, 16, kv_len, news, rng)
+    kv = fill_and_read(c, rng, kv_len, table)
+    for dtype in (torch.float32, torch.bfloat16):
+        q = rows(rng, (4, 71, 64), dtype)
+        for scale in (0.125, -0.2, 0.0):
+            out = c.attend(q, scale=scale)
+            check(c, q, out, out, kv, kv_len, news, scale)
+
+
+@gpu
+def test_scores_that_rise_and_fall():
+    """Running maxima that move with every token, by little and by much, and one token that takes it all."""
+    rng = np.random.default_rng(13)
+    n = 900
+    c, table = a_cache(1, 64, 16, [n], [1], rng)
+    v = torch.randn(n, 1, 64, device="cuda")
+    for name in ("up", "down", "saw", "peak"):
+        x = torch.linspace(-30, 30, n)
+        x = {"up": x, "down": -x, "saw": x * torch.where(torch.arange(n) % 7 < 3, 1.0, -1.0), "peak": torch.where(torch.arange(n) == 457, 200.0, 0.01 * x)}[name]
+        k = torch.randn(n, 1, 64, device="cuda") * 0.01
+        k[:, 0, 5] = x.cuda()
+        slots = slots_of(c, [n], table)
+        c.append(k, v, slots=torch.from_numpy(slots).cuda())
+        for dtype in (torch.float32, torch.bfloat16):
+            q = rows(rng, (1, 3, 64), dtype, 0.1)
+            q[0, :, 5] = torch.tensor([1.0, -3.0, 0.2])
+            out = c.attend(q, scale=1.0)
+            check(c, q, out, out, read_back(c, slots), [n], [1], 1.0)
 
 
 @gpu
