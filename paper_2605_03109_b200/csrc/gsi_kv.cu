@@ -736,7 +736,8 @@ gsi_status_t gsi_kv_attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t
   const gsi_status_t st = on_device(h);
   if (st != GSI_OK) return st;
   const kv::AttendArgs a{q, out, dtype, q_token_stride, q_head_stride, out_token_stride, out_head_stride, n_rows, n_q_heads,
-                         n_q_heads / h->shape.n_heads, 1.f / (n_q_heads / h->shape.n_heads), (float)(scale * 1.4426950408889634), q_start, kv_len, table, n_seqs, static_cast<const unsigned char*>(pages),
+                         n_q_heads / h->shape.n_heads, 1.f / (n_q_heads / h->shape.n_heads), aligned(q, 16) && ((q_token_stride | q_head_stride) * size_of(dtype) & 15) == 0,
+                         (float)(scale * 1.4426950408889634), q_start, kv_len, table, n_seqs, static_cast<const unsigned char*>(pages),
                          h->parts, h->tickets};
   return launched(h, stream, kv::launch_attend(h->shape, a, h->ctl, stream));
 }

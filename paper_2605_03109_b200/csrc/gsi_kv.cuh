@@ -83,6 +83,7 @@ struct AttendArgs {
   long long q_token, q_head, out_token, out_head;
   int n_rows, n_q_heads, shared;   // shared: q heads of a head of the cache (up to kMaxShared)
   float per_shared;                // 1 / shared
+  bool q_vec;                      // eight channels of q lie on 16 bytes
   float scale;   // of scores in powers of two
   const int *q_start, *kv_len, *table;
   int n_seqs;

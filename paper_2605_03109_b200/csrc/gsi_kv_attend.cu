@@ -34,16 +34,16 @@ using umma::s32;
 
 constexpr int kScan = 256;      // threads that look through the sequences
 constexpr int kGrid = 148;      // a block an SM (of two, the one that came first ran ahead by an eighth)
-constexpr int kFlush = 32;      // units between sums in fp32 (T = 2)
+constexpr int kFlush = 32;      // sets of tiles between sums in fp32 (T = 2)
 constexpr float kLow = 4096.f;  // units of the second term of q in one of the first
 constexpr float kLazy = 8.f;    // a running maximum is left where it is while 2^score stays below 2^kLazy above it
 constexpr float kOne = 64.f;    // p s <= 2^kLazy kOne s / vs < 2^15
 constexpr float kNone = -3e38f; // the maximum of no score
 
 // G: blocks of 64 channels; T: f16 terms of an operand; NT: column tiles of eight; L: lane quarters of a tile.
-// A unit of work is 4 / L tiles of tokens of one head and a tile of rows: the columns of a column tile are 2 L for each
-// of them, so that lane quarter t has the scores of tile t / L (rows t % L, T = 2; 2 (t % L) and the next, T = 1).
-// Few rows so share the scalar work of a tile's scores, where they would leave most columns empty.
+// The columns of a column tile are 2 L for each of 4 / L tiles of tokens, so that lane quarter t has the scores of tile t / L
+// (rows t % L, T = 2; 2 (t % L) and the next, T = 1).  Few rows so share the scalar work of a tile's scores, where they would
+// leave most columns empty.  A unit of work is one such set of tiles (two, where a set is one tile and the registers have room) of one head and a tile of rows.
 template <int G, int T, int L, int NT>
 struct Cfg {
   // Twelve warps where sixteen would leave too few registers: what is spilled comes back behind the tiles in flight.
@@ -51,7 +51,8 @@ struct Cfg {
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kShares = kGrid * kWarps;
   static constexpr int kDim = G * kGroup;
-  static constexpr int kTiles = 4 / L;                 // of a unit
+  static constexpr int kSet = 4 / L, kSets = L == 4 && G * NT <= 2 ? 2 : 1;   // tiles side by side in the columns, and one after the other
+  static constexpr int kTiles = kSet * kSets;          // of a unit
   static constexpr int kLaneRows = T == 1 ? 2 : 1;     // rows of a lane per column tile
   static constexpr int kRows = NT * L * kLaneRows;     // rows of a unit
   static constexpr int kHalf = G * kBlockBytes;        // K of a tile, or V
@@ -68,7 +69,7 @@ struct Cfg {
   static constexpr int kSmem = kWarps * kWarpBytes;
   static_assert(kShares <= kMaxShares, "the workspace's parts and tickets");
   static constexpr int kSnap = kTiles == 1 ? 2 : 1;    // units: the share of a warp ends with a segment that ends as near
-  static constexpr int kCost = L + 1;                    // units that a segment itself counts as in a share
+  static constexpr int kCost = kSets == 2 ? 3 : L + 1;                    // units that a segment itself counts as in a share
   static constexpr int kPart = kPartFloats(G);
   static constexpr int kPartRows = kPart / (kDim + 8);
 };
@@ -184,7 +185,7 @@ struct Pending {
 template <int G, int T, int L, int NT>
 __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Shape s, AttendArgs a, Control* ctl) {
   using C = Cfg<G, T, L, NT>;
-  constexpr int kLR = C::kLaneRows, N = C::kTiles, kWarps = C::kWarps, kThreads = C::kThreads;
+  constexpr int kLR = C::kLaneRows, N = C::kTiles, kSet = C::kSet, kSets = C::kSets, kWarps = C::kWarps, kThreads = C::kThreads;
   static_assert(C::kRing >= (int)sizeof(Scan2) * kScan, "prefixes lie in the first warp's rings");
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ Scan2 s_warp[kWarps];
@@ -279,18 +280,38 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
       row_tile = first - head * q.n_row_tiles;
     }
 
-    // The first row of q is asked for ahead of the tiles, which would hold it up; rows of later segments are prefetched.
-    uint32_t q_first[2 * G];   // as it lies there
-    auto fetch = [&](long long from, uint32_t (&v)[2 * G]) {
+    // Rows of q: a lane takes eight channels, a word of K's codes, kRowLanes lanes a row.  The first ones are asked for ahead of the
+    // tiles, which would hold them up; rows of later segments are prefetched.
+    constexpr int kRowLanes = G == 1 ? 8 : G == 2 ? 16 : 32, kRowsAtOnce = 32 / kRowLanes;
+    const int my_word = lane % kRowLanes, my_row = lane / kRowLanes;
+    uint32_t q_raw[T == 2 ? 8 : 4];   // as they lie there
+    auto fetch = [&](long long from, bool there) {
 #pragma unroll
-      for (int i = 0; i < 2 * G; ++i) {
-        const int c = i * 32 + lane;
-        v[i] = 0u;
-        if (c < s.head_dim) v[i] = T == 2 ? static_cast<const uint32_t*>(a.q)[from + c] : static_cast<const uint16_t*>(a.q)[from + c];
+      for (int i = 0; i < (T == 2 ? 8 : 4); ++i) q_raw[i] = 0u;
+      const int n = there ? s.head_dim - my_word * 8 : 0;
+      from += my_word * 8;
+      if (n >= 8 && a.q_vec) {
+        const uint4* at = reinterpret_cast<const uint4*>(static_cast<const char*>(a.q) + from * (T == 2 ? 4 : 2));
+        const uint4 v = at[0];
+        q_raw[0] = v.x, q_raw[1] = v.y, q_raw[2] = v.z, q_raw[3] = v.w;
+        if constexpr (T == 2) {
+          const uint4 y = at[1];
+          q_raw[4] = y.x, q_raw[5] = y.y, q_raw[6] = y.z, q_raw[7] = y.w;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n) {
+            if constexpr (T == 2) q_raw[i] = static_cast<const uint32_t*>(a.q)[from + i];
+            else q_raw[i / 2] |= (uint32_t)static_cast<const uint16_t*>(a.q)[from + i] << 16 * (i & 1);
+          }
       }
     };
-    auto as_float = [&](uint32_t v) {
-      return T == 2 ? __uint_as_float(v) : a.dtype == GSI_BF16 ? __uint_as_float(v << 16) : __half2float(__ushort_as_half((unsigned short)v));
+    auto channel = [&](int i) {
+      if (T == 2) return __uint_as_float(q_raw[i]);
+      const uint32_t w = q_raw[i / 2 % (T == 2 ? 8 : 4)];
+      if (a.dtype == GSI_BF16) return __uint_as_float((i & 1) ? w & 0xFFFF0000u : w << 16);
+      return __half2float(__ushort_as_half((unsigned short)(w >> 16 * (i & 1))));
     };
     // row r of a tile of rows, from the step's row `step0` and the q head `in0` of those that share the head on
     auto step_of = [&](int in0, int r) { return __float2int_rd((in0 + r + 0.5f) * a.per_shared); };
@@ -300,7 +321,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
     };
     if (mine > 0) {
       const int row0 = row_tile * C::kRows, step0 = row0 / a.shared;
-      fetch(q_from(q, head, step0, row0 - step0 * a.shared, 0), q_first);
+      fetch(q_from(q, head, step0, row0 - step0 * a.shared, my_row), my_row < min(C::kRows, q.m * a.shared - row0));
     }
 
     // ---- its tiles come through a ring; lane (N j + i) % 32 knows where tile i of unit j lies
@@ -336,15 +357,15 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
     bool gave_up = false;    // a copy did not arrive
 
     // what of the columns' operands is of tile i: the columns of the others are zero
-    uint32_t only[N];
-    uint32_t q_at[N];
+    uint32_t only[kSet];
+    uint32_t q_at[kSet];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i < kSet; ++i) {
       const bool of = gr / (2 * L) == i;
       only[i] = of ? ~0u : 0u;
-      q_at[i] = s32(s_q) + ((N == 1 || of ? gr % (2 * L) : 2 * L) * 4 + t4) * 16;
+      q_at[i] = s32(s_q) + ((kSet == 1 || of ? gr % (2 * L) : 2 * L) * 4 + t4) * 16;
     }
-    const int my_tile = t4 / L;   // the one whose scores this lane has
+    const int my_tile = t4 / L;   // the one of a set whose scores this lane has
     const uint32_t ring_at = s32(ring), start_at = s32(s_start), sum_at = s32(s_sum);
     const uint32_t my_pair = my_tile * C::kStride + kCodeBytes + gr * 8, my_codes = lane * 16;
     const uint32_t my_slot = ring_at + lane % N * C::kStride, my_bar = s32(bars);   // where its copies go, and their barriers
@@ -377,37 +398,42 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
       auto q_head = [&](int r) { return head * a.shared + row0 + r - step_row(r) * a.shared; };
       auto sees = [&](int r) { return q.seen + step_row(min(r, n_rows - 1)) + 1; };
 
-      // the rows as B operand, a lane 2 G channels.  (Columns of rows that are not there hold what they held.)
-      for (int r = 0; r < n_rows; ++r) {
-        if (j && r == 0) fetch(q_from(q, head, step0, in0, 0), q_first);
-        float v[2 * G], top = 0.f;
+      // the rows as B operand.  (Columns of rows that are not there hold what they held.)
+      for (int r0 = 0; r0 < n_rows; r0 += kRowsAtOnce) {
+        const int r = r0 + my_row;
+        if (j && r0 == 0) fetch(q_from(q, head, step0, in0, r), r < n_rows);
+        float v[8], top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 2 * G; ++i) {
-          v[i] = as_float(q_first[i]);
+        for (int i = 0; i < 8; ++i) {
+          v[i] = channel(i);
           top = fmaxf(top, fabsf(v[i]));
         }
-        if (r + 1 < n_rows) fetch(q_from(q, head, step0, in0, r + 1), q_first);
+        if (r0 + kRowsAtOnce < n_rows) fetch(q_from(q, head, step0, in0, r + kRowsAtOnce), r + kRowsAtOnce < n_rows);
 #pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        for (int o = kRowLanes / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         // 2^k takes the largest to below 2^11 (2^14), as a product of two; a row of zeros, or with an infinity, stays as it is
         int k = (T == 2 ? 137 : 140) - (int)(__float_as_uint(top) >> 23);
         if (top == 0.f || top > 3.402823466e38f) k = 0;
         const float k0 = __uint_as_float((uint32_t)(127 + k / 2) << 23), k1 = __uint_as_float((uint32_t)(127 + k - k / 2) << 23);
+        float lo[8];
 #pragma unroll
-        for (int i = 0; i < 2 * G; ++i) {
-          const int c = (i & 1) * 32 + lane, g = i >> 1, nib = c & 7;   // channel of the block, of its word
-          const float x = v[i] * k0 * k1;
-          const float odd = (nib & 1) ? 0.0625f : 1.f, hi = T == 2 ? rintf(x) : x, lo = T == 2 ? rintf((x - hi) * kLow) : 0.f;
-          // word (c % 16) / 8 of lane c / 16: its two steps' registers (nib / 2) % 2, b0 or b1 nib % 2, half nib / 4
-          const int col = T == 2 ? r % L * 2 : r % (2 * L), nt = T == 2 ? r / L : r / (2 * L);
-          __half* to = reinterpret_cast<__half*>(s_q + ((nt * G + g) * 2 + (c % 16) / 8) * 512 + (col * 4 + c / 16) * 16) + (nib / 2 % 2) * 4 +
-                       (nib & 1) * 2 + nib / 4;
-          *to = __float2half_rn(hi * odd);
-          if constexpr (T == 2) to[32] = __float2half_rn(lo * odd);   // the next column: 4 lanes of 16 bytes on
+        for (int i = 0; i < 8; ++i) {
+          const float x = v[i] * k0 * k1, odd = (i & 1) ? 0.0625f : 1.f;   // (codes of odd channels enter as 16 code)
+          v[i] = T == 2 ? rintf(x) : x;
+          lo[i] = T == 2 ? rintf((x - v[i]) * kLow) * odd : 0.f;
+          v[i] *= odd;
         }
-        // (powers of two: 2^(24 - k) in two steps)
-        const float back0 = __uint_as_float((uint32_t)(127 - k / 2) << 23), back1 = __uint_as_float((uint32_t)(151 - k + k / 2) << 23);
-        if (lane == 0) s_factor[r] = fminf(fmaxf(a.scale * back0 * back1, -0x1p100f), 0x1p100f);
+        if (r < n_rows && my_word < 8 * G) {
+          // channels i and i + 4 of word h of lane t: of its two steps, registers b0 and b1
+          const int col = T == 2 ? r % L * 2 : r % (2 * L), nt = T == 2 ? r / L : r / (2 * L);
+          uint4* to = reinterpret_cast<uint4*>(s_q + ((nt * G + my_word / 8) * 2 + my_word % 2) * 512 + (col * 4 + my_word % 8 / 2) * 16);
+          to[0] = make_uint4(pack_half2(v[0], v[4]), pack_half2(v[1], v[5]), pack_half2(v[2], v[6]), pack_half2(v[3], v[7]));
+          if constexpr (T == 2)   // the next column
+            to[4] = make_uint4(pack_half2(lo[0], lo[4]), pack_half2(lo[1], lo[5]), pack_half2(lo[2], lo[6]), pack_half2(lo[3], lo[7]));
+          // (powers of two: 2^(24 - k) in two steps)
+          const float back0 = __uint_as_float((uint32_t)(127 - k / 2) << 23), back1 = __uint_as_float((uint32_t)(151 - k + k / 2) << 23);
+          if (my_word == 0) s_factor[r] = fminf(fmaxf(a.scale * back0 * back1, -0x1p100f), 0x1p100f);
+        }
       }
       __syncwarp();
       // Per block, what the scores' sums begin with, -8 times the sum of the column's q (the sums are then those of
@@ -486,13 +512,16 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
       // A unit from token `first_pos` on; masked: where some row does not see all of it, or a page is missing (a bit for each tile)
       auto pass = [&](auto is_masked, int first_pos, unsigned missing, int next) {
         constexpr bool kMasked = decltype(is_masked)::value;
-        const int pos = first_pos + my_tile * kTile + gr;
-        const bool wrong = kMasked && (missing >> my_tile & 1u);
-        float S[NT][kLR][2], p[NT][kLR][2];
+        const int pos = first_pos + my_tile * kTile + gr;   // of the first set
+        bool wrong[kSets];
+        float S[kSets][NT][kLR][2], p[kSets][NT][kLR][2];
         const uint32_t k_at = ring_at + stage * N * C::kStride, v_at = k_at + C::kToV;
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          const uint2 pw = lds64(k_at + my_pair + g * kBlockBytes);
+        for (int u = 0; u < kSets; ++u) {
+          wrong[u] = kMasked && (missing >> (u * kSet + my_tile) & 1u);
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+          const uint2 pw = lds64(k_at + my_pair + (u * kSet * C::kStride + g * kBlockBytes));
           float acc[NT][4];
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
@@ -507,8 +536,8 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
             }
           }
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const uint4 w = lds128(k_at + my_codes + (i * C::kStride + g * kBlockBytes));
+          for (int i = 0; i < kSet; ++i) {
+            const uint4 w = lds128(k_at + my_codes + ((u * kSet + i) * C::kStride + g * kBlockBytes));
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const uint32_t x = h ? w.y : w.x, y = h ? w.w : w.z;
@@ -529,9 +558,10 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
               const float qs = lds_float(sum_at + (g * C::kRows + row_of(n, r)) * 4);
               const float a0 = T == 2 ? fmaf(acc[n][1], 1.f / kLow, acc[n][0]) : acc[n][r];
               const float a1 = T == 2 ? fmaf(acc[n][3], 1.f / kLow, acc[n][2]) : acc[n][2 + r];
-              S[n][r][0] = fmaf(p0.x, a0, g ? fmaf(p0.y, qs, S[n][r][0]) : p0.y * qs);
-              S[n][r][1] = fmaf(p1.x, a1, g ? fmaf(p1.y, qs, S[n][r][1]) : p1.y * qs);
+              S[u][n][r][0] = fmaf(p0.x, a0, g ? fmaf(p0.y, qs, S[u][n][r][0]) : p0.y * qs);
+              S[u][n][r][1] = fmaf(p1.x, a1, g ? fmaf(p1.y, qs, S[u][n][r][1]) : p1.y * qs);
             }
+          }
         }
         if constexpr (C::kSplit) {
           __syncwarp();
@@ -542,34 +572,40 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           }
         }
         // pairs of V, and their largest step
-        uint2 pv[G];
+        uint2 pv[kSets][G];
         __half2 steps = __half2half2(__ushort_as_half(0));
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          pv[g] = lds64(v_at + my_pair + g * kBlockBytes);
-          if constexpr (kMasked) {   // (behind the last token lies anything)
-            if (wrong || pos >= q.len) pv[g].x = 0u;
-            if (wrong || pos + 8 >= q.len) pv[g].y = 0u;
+        for (int u = 0; u < kSets; ++u)
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            uint2& v = pv[u][g];
+            v = lds64(v_at + my_pair + (u * kSet * C::kStride + g * kBlockBytes));
+            if constexpr (kMasked) {   // (behind the last token lies anything)
+              const int at = pos + u * kSet * kTile;
+              if (wrong[u] || at >= q.len) v.x = 0u;
+              if (wrong[u] || at + 8 >= q.len) v.y = 0u;
+            }
+            steps = __hmax2(steps, __hmax2(*reinterpret_cast<const __half2*>(&v.x), *reinterpret_cast<const __half2*>(&v.y)));
           }
-          steps = __hmax2(steps, __hmax2(*reinterpret_cast<const __half2*>(&pv[g].x), *reinterpret_cast<const __half2*>(&pv[g].y)));
-        }
         const float step = __low2float(steps);
         bool move = step > vs;
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int u = 0; u < kSets; ++u)
 #pragma unroll
-          for (int r = 0; r < kLR; ++r) {
-            if constexpr (kMasked) {   // (scaled here: a factor of 0, or below, would make something else of infinity)
-              const int vis = sees(row_of(n, r)) - pos;
-              S[n][r][0] = vis <= 0 ? -INFINITY : wrong ? NAN : S[n][r][0] * factor[n][r];
-              S[n][r][1] = vis <= 8 ? -INFINITY : wrong ? NAN : S[n][r][1] * factor[n][r];
-            }
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              p[n][r][e] = fmaf(S[n][r][e], kMasked ? 1.f : factor[n][r], -m[n][r]);
-              move = move || p[n][r][e] > kLazy;
+            for (int r = 0; r < kLR; ++r) {
+              if constexpr (kMasked) {   // (scaled here: a factor of 0, or below, would make something else of infinity)
+                const int vis = sees(row_of(n, r)) - pos - u * kSet * kTile;
+                S[u][n][r][0] = vis <= 0 ? -INFINITY : wrong[u] ? NAN : S[u][n][r][0] * factor[n][r];
+                S[u][n][r][1] = vis <= 8 ? -INFINITY : wrong[u] ? NAN : S[u][n][r][1] * factor[n][r];
+              }
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                p[u][n][r][e] = fmaf(S[u][n][r][e], kMasked ? 1.f : factor[n][r], -m[n][r]);
+                move = move || p[u][n][r][e] > kLazy;
+              }
             }
-          }
         if (__any_sync(0xffffffffu, move)) {
           float largest = step;
 #pragma unroll
@@ -584,7 +620,9 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
 #pragma unroll
             for (int r = 0; r < kLR; ++r) {
               const float f = kMasked ? 1.f : factor[n][r];
-              float x = fmaxf(m[n][r], fmaxf(S[n][r][0] * f, S[n][r][1] * f));
+              float x = m[n][r];
+#pragma unroll
+              for (int u = 0; u < kSets; ++u) x = fmaxf(x, fmaxf(S[u][n][r][0] * f, S[u][n][r][1] * f));
 #pragma unroll
               for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
               if (x - m[n][r] <= kLazy) x = m[n][r];   // (another row's: this one's sums stay as they are)
@@ -595,7 +633,9 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
               for (int g = 0; g < G; ++g) z[n][r][g] *= keep[n][r];
               keep[n][r] *= v_keep;
 #pragma unroll
-              for (int e = 0; e < 2; ++e) p[n][r][e] = fmaf(S[n][r][e], f, -x);
+              for (int u = 0; u < kSets; ++u)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) p[u][n][r][e] = fmaf(S[u][n][r][e], f, -x);
             }
 #pragma unroll
           for (int n = 0; n < NT; ++n)
@@ -606,6 +646,8 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
 #pragma unroll
                 for (int e = 0; e < 4; ++e) O[n][g][i][e] *= keep[n][kLR == 2 ? e & 1 : 0];
         }
+#pragma unroll
+        for (int u = 0; u < kSets; ++u) {
         float ps[NT][kLR][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -613,13 +655,13 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           for (int r = 0; r < kLR; ++r)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              p[n][r][e] = exp2_fast(p[n][r][e]);
-              l[n][r] += p[n][r][e];
-              ps[n][r][e] = p[n][r][e] * vinv;
+              p[u][n][r][e] = exp2_fast(p[u][n][r][e]);
+              l[n][r] += p[u][n][r][e];
+              ps[n][r][e] = p[u][n][r][e] * vinv;
             }
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          const float2 p0 = unpack_half2(pv[g].x), p1 = unpack_half2(pv[g].y);
+          const float2 p0 = unpack_half2(pv[u][g].x), p1 = unpack_half2(pv[u][g].y);
           uint32_t b0[NT], b1[NT];
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
@@ -629,13 +671,13 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
               x[r][0] = ps[n][r][0] * p0.x;
               x[r][1] = ps[n][r][1] * p1.x;
               if constexpr (kMasked) {   // (a token that this row does not see need not be a number)
-                const int vis = sees(row_of(n, r)) - pos;
+                const int vis = sees(row_of(n, r)) - pos - u * kSet * kTile;
                 if (vis <= 0) x[r][0] = 0.f;
-                else z[n][r][g] = fmaf(p[n][r][0], p0.y, z[n][r][g]);
+                else z[n][r][g] = fmaf(p[u][n][r][0], p0.y, z[n][r][g]);
                 if (vis <= 8) x[r][1] = 0.f;
-                else z[n][r][g] = fmaf(p[n][r][1], p1.y, z[n][r][g]);
+                else z[n][r][g] = fmaf(p[u][n][r][1], p1.y, z[n][r][g]);
               } else {
-                z[n][r][g] = fmaf(p[n][r][1], p1.y, fmaf(p[n][r][0], p0.y, z[n][r][g]));
+                z[n][r][g] = fmaf(p[u][n][r][1], p1.y, fmaf(p[u][n][r][0], p0.y, z[n][r][g]));
               }
             }
             if constexpr (T == 2) {   // its upper eleven bits and the rest
@@ -650,8 +692,8 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
             b1[n] = transpose8x8(b1[n]);
           }
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const uint4 w = lds128(v_at + my_codes + (i * C::kStride + g * kBlockBytes));
+          for (int i = 0; i < kSet; ++i) {
+            const uint4 w = lds128(v_at + my_codes + ((u * kSet + i) * C::kStride + g * kBlockBytes));
             const uint32_t x8 = w.x >> 8, y8 = w.y >> 8, z8 = w.z >> 8, w8 = w.w >> 8;
             const uint32_t A[4][4] = {{centred<false>(w.x), centred<false>(w.y), centred<false>(w.z), centred<false>(w.w)},
                                       {centred<true>(w.x), centred<true>(w.y), centred<true>(w.z), centred<true>(w.w)},
@@ -659,11 +701,12 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
                                       {centred<true>(x8), centred<true>(y8), centred<true>(z8), centred<true>(w8)}};
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              const uint32_t c0 = N == 1 ? b0[n] : b0[n] & only[i], c1 = N == 1 ? b1[n] : b1[n] & only[i];
+              const uint32_t c0 = kSet == 1 ? b0[n] : b0[n] & only[i], c1 = kSet == 1 ? b1[n] : b1[n] & only[i];
 #pragma unroll
               for (int k = 0; k < 4; ++k) mma_f16(O[n][g][k], A[k][0], A[k][1], A[k][2], A[k][3], c0, c1);
             }
           }
+        }
         }
       };
 
@@ -715,7 +758,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           phase ^= 1u;
         }
         ++j;
-        if (T == 2 && ++since == kFlush && j < end) {
+        if (T == 2 && (since += kSets) >= kFlush && j < end) {
           since = 0;
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
