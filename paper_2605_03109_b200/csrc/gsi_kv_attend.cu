@@ -319,7 +319,16 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
       const int i = step_of(in0, r);
       return (long long)(x.q0 + step0 + i) * a.q_token + (long long)(of_head * a.shared + in0 + r - i * a.shared) * a.q_head;
     };
+    auto prefetch = [&](const Seq& x, int of_head, int of_tile) {
+      const int row0 = of_tile * C::kRows, n = min(C::kRows, x.m * a.shared - row0), step0 = row0 / a.shared;
+      constexpr int kLines = G * 2 / T;   // of 128 bytes, a row
+      for (int i = lane; i < n * kLines; i += 32) {
+        const char* at = static_cast<const char*>(a.q) + q_from(x, of_head, step0, row0 - step0 * a.shared, i / kLines) * (T == 2 ? 4 : 2) + i % kLines * 128;
+        if (i % kLines * (T == 2 ? 32 : 64) < s.head_dim) asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+      }
+    };
     if (mine > 0) {
+      if (C::kRows > kRowsAtOnce) prefetch(q, head, row_tile);
       const int row0 = row_tile * C::kRows, step0 = row0 / a.shared;
       fetch(q_from(q, head, step0, row0 - step0 * a.shared, my_row), my_row < min(C::kRows, q.m * a.shared - row0));
     }
@@ -476,13 +485,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
             while (x.n_row_tiles == 0);
           }
         }
-        const int first = x_tile * C::kRows, n = min(C::kRows, x.m * a.shared - first), x_step = first / a.shared;
-        constexpr int kLines = G * 2 / T;   // of 128 bytes, a row
-        for (int i = lane; i < n * kLines; i += 32) {
-          const char* at = static_cast<const char*>(a.q) +
-                           q_from(x, x_head, x_step, first - x_step * a.shared, i / kLines) * (T == 2 ? 4 : 2) + i % kLines * 128;
-          if (i % kLines * (T == 2 ? 32 : 64) < s.head_dim) asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
-        }
+        prefetch(x, x_head, x_tile);
       }
 
       // sums and maxima, of each tile of a unit its own until the segment ends
