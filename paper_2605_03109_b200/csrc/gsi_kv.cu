@@ -46,7 +46,8 @@ __device__ __forceinline__ bool read_last(Control* ctl, int* s_last) {
 // Every block works the requests' sums out for itself (2048 requests: 16 KB from the L2), so that no block waits for
 // another; the sequences' first rows and first pages stay in shared memory, where each run of tokens and each page of the
 // block looks up its own.  The block that is last to have read the state moves it on.
-// Bound by the launch and three dependent reads (one token: 4.1 us a call); for prompts by the writes of slots and positions.
+// Bound by the launch and three dependent reads (one token or 64: 3.0-3.4 us a call); prompts of 512 requests, 2.05 million tokens,
+// take 13 us, 3 of them the slots' and positions' bytes.
 template <int kRun>
 __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, Control* ctl) {
   extern __shared__ int sm[];
@@ -376,8 +377,8 @@ __device__ __forceinline__ unsigned char* block_of(const Shape& s, unsigned char
   return pages + tile_at(s, page, it.head, in / kTile) + it.group * kBlockBytes;
 }
 
-// K and V of a row are under way together.  Bound by issue for long prompts (about 15 instructions a channel and lane), not far above
-// the rows' bytes.
+// K and V of a row are under way together.  Bound by issue for long prompts, 25 instructions a channel and lane: 16001 rows of 32 heads
+// of 128 take 125 us in bf16 (2.7 TB/s), 8000 in fp32 64 us (4.7 TB/s).
 template <gsi_dtype_t kType, bool kVec>
 __global__ void __launch_bounds__(kRowWarps * 32, kType == GSI_F32 ? 7 : 8) k_kv_append(Shape s, RowsArgs a, Control* ctl) {
   const int quarter = threadIdx.x & 3;
@@ -443,7 +444,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, kType == GSI_F32 ? 7 : 8) k_kv
   }
 }
 
-// A lane quarter takes channels 4 t + 16 i .. + 3, so that four lanes write 64 (32) bytes in one go.
+// A lane quarter takes channels 4 t + 16 i .. + 3, so that four lanes write 64 (32) bytes in one go: 16001 rows of 32 heads of 128 to
+// fp32 in 102 us, 5.8 TB/s.
 template <gsi_dtype_t kType, bool kVec>
 __global__ void __launch_bounds__(kRowWarps * 32) k_kv_read(Shape s, RowsArgs a, Control* ctl) {
   const int quarter = threadIdx.x & 3;
