@@ -675,6 +675,57 @@ def test_a_captured_step_moves_on_by_itself():
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_captured_attention_goes_by_the_lengths_of_its_replay(dtype):
+    """Captured with short requests, replayed with long ones, and the other way round."""
+    rng = np.random.default_rng(21)
+    long, short, news = [5000, 1, 700, 0], [3, 40, 0, 17], [2, 1, 1, 1]
+    for first, then in ((short, long), (long, short)):
+        c, table = a_cache(2, 128, 16, [max(a, b) for a, b in zip(long, short)], news, rng)
+        kv = fill_and_read(c, rng, [max(a, b) for a, b in zip(long, short)], table)
+        at = np.concatenate([[0], np.cumsum([max(a, b) for a, b in zip(long, short)])])
+        q = rows(rng, (6, 4, 128), dtype)
+        out = torch.zeros_like(q)
+        c.kv_len.copy_(ints(first))
+        c.attend(q, out=out)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            c.attend(q, out=out)
+        for lens in (then, first, then):
+            c.kv_len.copy_(ints(lens))
+            out.fill_(9.0)
+            before = out.clone()
+            graph.replay()
+            of = [[np.concatenate([x[at[i]:at[i] + n] for i, n in enumerate(lens)]) for x in z] for z in kv]
+            check(c, q, out, before, of, lens, news, 128 ** -0.5)
+            assert torch.equal(c.attend(q)[:5], out[:5])
+        assert c.status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("n_seqs,page,heads", [(2048, 16, 1), (3, 4096, 2), (17, 112, 3)])
+def test_the_ends_of_the_sizes(n_seqs, page, heads):
+    """As many requests as there can be, the largest pages, pages whose tiles are no power of two; planned, not laid out here."""
+    g, rng = gsi(), np.random.default_rng(n_seqs)
+    n_new = rng.integers(0, 2 * page if n_seqs < 100 else 20, n_seqs)
+    c = g.KVCache(heads, 64, int(sum(-(-n // page) for n in n_new)) + n_seqs, n_seqs, 3 * page, page_tokens=page, max_tokens=int(n_new.sum()),
+                  pages=torch.full((int(sum(-(-n // page) for n in n_new)) + n_seqs, heads * page * 72), 0xFF, dtype=torch.uint8, device="cuda"))
+    c.plan(ints(n_new.tolist()))
+    n = int(n_new.sum())
+    k, v = (torch.randn(n, heads, 64, device="cuda") for _ in range(2))
+    c.append(k, v)
+    c.plan(ints([1] * n_seqs), commit=False)
+    more = [torch.randn(n_seqs, heads, 64, device="cuda") for _ in range(3)]
+    c.append(more[1], more[2])
+    out = c.attend(more[0])
+    lens = (n_new + 1).tolist()
+    table = c.table.cpu().numpy().astype(np.int64)
+    check(c, more[0], out, out, read_back(c, slots_of(c, lens, table)), lens, [1] * n_seqs, 0.125)
+    assert c.status() == 0
+
+
+@gpu
 def test_streams_of_their_own():
     """Two caches on two streams at once, each with its own workspace, against one after the other."""
     rng = np.random.default_rng(11)
