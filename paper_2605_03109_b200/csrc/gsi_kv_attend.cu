@@ -212,63 +212,115 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
     for (int i = 0; i < C::kBars / 8; ++i) mbar_init(bars + i, N);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   if (tid == 0) s_n_pending = 0;
+  __syncthreads();
   pdl_launch_dependents();
   pdl_wait();
 
-  // ---- shares: the units of all sequences in order, in even pieces that end with a segment where one ends near
-  const int per = (a.n_seqs + kScan - 1) / kScan;
-  Scan2 sum{0, 0}, total;
-  for (int i = tid * per; tid < kScan && i < min(tid * per + per, a.n_seqs); ++i) {
-    const Seq x = load(i);
-    sum.a += x.all(s);
-    sum.b += x.segments(s);
-  }
-  for (int i = lane; i < (C::kQ + C::kSums) / 16; i += 32) reinterpret_cast<uint4*>(s_q)[i] = make_uint4(0u, 0u, 0u, 0u);
-  const Scan2 before = block_scan(sum, &total, s_warp);
-  if (tid < kScan) s_before[tid] = before;
-  if (total.a == 0) return;
-  // (a segment counts as kCost units more: its rows have to be fetched and its sums to be put away)
-  const long long weight = total.a + C::kCost * total.b;
-  const long long shares = max(1ll, min((long long)C::kShares, max(quotient(weight, C::kSnap + C::kCost), total.b)));
+  // ---- shares: the units of all sequences in order, in even pieces that end with a segment where one ends near.  A segment
+  // counts as kCost units more: its rows have to be fetched and its sums to be put away.
+  Scan2 total;
+  long long weight, shares;
+  bool full;
+  int my_share, stride;
   // Few shares: one a block.  Otherwise a block's are neighbours: long segments are then the work of a few blocks each, and
   // not all of them wait for the slowest one.
-  const bool full = shares == C::kShares;
-  const int my_share = full ? blockIdx.x * kWarps : blockIdx.x, stride = full ? 1 : kGrid;
-  if (my_share >= shares) return;
-  __syncthreads();
-  if (tid < kWarps * 2) {   // the shares of the block's warps, and those behind them
-    const long long x = quotient(weight * (my_share + (tid >> 1) * stride + (tid & 1)), shares);
-    Begin at{total.a, 0, 0, 0};
-    if (x < weight) {
-      int lo = 0, hi = kScan;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (s_before[mid].a + C::kCost * s_before[mid].b <= x) lo = mid;
-        else hi = mid;
-      }
-      at = {0, s_before[lo].a, s_before[lo].b, lo * per};
-      Seq q = load(at.seq);
-      for (;;) {
-        const long long n = q.segments(s);
-        if (x < at.base + C::kCost * at.segments + n * (q.units + C::kCost)) break;
-        at.base += n * q.units;
-        at.segments += n;
-        q = load(++at.seq);
-      }
-      const long long in = x - at.base - C::kCost * at.segments, segment = quotient(in, q.units + C::kCost);
-      const int unit = max((int)(in - segment * (q.units + C::kCost)) - C::kCost, 0), left = q.units - unit;
-      at.u = at.base + segment * q.units + (unit < C::kSnap && unit <= left ? 0 : left < C::kSnap ? q.units : unit);
+  auto share_out = [&]() {
+    weight = total.a + C::kCost * total.b;
+    shares = max(1ll, min((long long)C::kShares, max(quotient(weight, C::kSnap + C::kCost), total.b)));
+    full = shares == C::kShares;
+    my_share = full ? blockIdx.x * kWarps : blockIdx.x;
+    stride = full ? 1 : kGrid;
+  };
+  // the first unit of the share that begins at x of a sequence's weight, from the sequence's first on
+  auto unit_at = [&](long long x, int units) {
+    const long long segment = quotient(x, units + C::kCost);
+    const int unit = max((int)(x - segment * (units + C::kCost)) - C::kCost, 0), left = units - unit;
+    return segment * units + (unit < C::kSnap && unit <= left ? 0 : left < C::kSnap ? units : unit);
+  };
+  auto clear_rows = [&]() {   // (while the lengths are on their way)
+    for (int i = lane; i < (C::kQ + C::kSums) / 16; i += 32) reinterpret_cast<uint4*>(s_q)[i] = make_uint4(0u, 0u, 0u, 0u);
+  };
+  long long u0 = 0, u1 = 0, base = 0, segment = 0;   // the warp's units; its first sequence's first unit; the next segment, counted over all sequences
+  int seq = 0;
+  if (a.n_seqs <= 32) {   // a lane a sequence, no wait between the warps (12 heads of 64, 33 tokens: 7.5 -> 6.8 us; up to
+                          // 128 sequences, four a lane: no gain)
+    Scan2 mine{0, 0};
+    int units = 1;
+    if (lane < a.n_seqs) {
+      const Seq x = load(lane);
+      mine = {x.all(s), x.segments(s)};
+      units = x.units;
     }
-    s_begin[tid] = at;
+    clear_rows();
+    Scan2 upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long na = __shfl_up_sync(0xffffffffu, upto.a, o), nb = __shfl_up_sync(0xffffffffu, upto.b, o);
+      if (lane >= o) upto = {upto.a + na, upto.b + nb};
+    }
+    total = {__shfl_sync(0xffffffffu, upto.a, 31), __shfl_sync(0xffffffffu, upto.b, 31)};
+    if (total.a == 0) return;
+    share_out();
+    if (my_share >= shares) return;
+    const Scan2 before{upto.a - mine.a, upto.b - mine.b};
+    const long long from = before.a + C::kCost * before.b;
+#pragma unroll
+    for (int e = 1; e >= 0; --e) {
+      const long long x = quotient(weight * min((long long)my_share + warp * stride + e, shares), shares);
+      // the last sequence that begins there or before (of those without units, which begin where the next one does, none is the last)
+      const int at = 31 - __clz(__ballot_sync(0xffffffffu, lane < a.n_seqs && from <= x));
+      base = __shfl_sync(0xffffffffu, before.a, at);
+      segment = __shfl_sync(0xffffffffu, before.b, at);
+      const long long u = x >= weight ? total.a : base + unit_at(x - base - C::kCost * segment, __shfl_sync(0xffffffffu, units, at));
+      (e ? u1 : u0) = u;
+      seq = at;
+    }
+  } else {
+    const int per = (a.n_seqs + kScan - 1) / kScan;
+    Scan2 sum{0, 0};
+    for (int i = tid * per; tid < kScan && i < min(tid * per + per, a.n_seqs); ++i) {
+      const Seq x = load(i);
+      sum.a += x.all(s);
+      sum.b += x.segments(s);
+    }
+    clear_rows();
+    const Scan2 before = block_scan(sum, &total, s_warp);
+    if (tid < kScan) s_before[tid] = before;
+    if (total.a == 0) return;
+    share_out();
+    if (my_share >= shares) return;
+    __syncthreads();
+    if (tid < kWarps * 2) {   // the shares of the block's warps, and those behind them
+      const long long x = quotient(weight * (my_share + (tid >> 1) * stride + (tid & 1)), shares);
+      Begin at{total.a, 0, 0, 0};
+      if (x < weight) {
+        int lo = 0, hi = kScan;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (s_before[mid].a + C::kCost * s_before[mid].b <= x) lo = mid;
+          else hi = mid;
+        }
+        at = {0, s_before[lo].a, s_before[lo].b, lo * per};
+        Seq q = load(at.seq);
+        for (;;) {
+          const long long n = q.segments(s);
+          if (x < at.base + C::kCost * at.segments + n * (q.units + C::kCost)) break;
+          at.base += n * q.units;
+          at.segments += n;
+          q = load(++at.seq);
+        }
+        at.u = at.base + unit_at(x - at.base - C::kCost * at.segments, q.units);
+      }
+      s_begin[tid] = at;
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    const Begin& at = s_begin[warp * 2];
+    u0 = at.u, u1 = s_begin[warp * 2 + 1].u, base = at.base, segment = at.segments, seq = at.seq;
   }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  __syncthreads();
   const int share = my_share + warp * stride;
 
   if (share < shares) {
-    const long long u0 = s_begin[warp * 2].u, u1 = s_begin[warp * 2 + 1].u;
-    long long base = s_begin[warp * 2].base, segment = s_begin[warp * 2].segments;   // the next one, counted over all sequences
-    int seq = s_begin[warp * 2].seq;
     const int mine = (int)(u1 - u0);   // the warp's units
     Seq q;
     int head = 0, row_tile = 0, unit = 0;   // of the next unit
