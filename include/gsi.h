@@ -484,7 +484,8 @@ typedef struct {
   int max_tokens;  /* new tokens of a step: the length of slots and positions       */
 } gsi_kv_desc_t;
 
-/* Bytes of one page of one pool, of the workspace (0 if desc is invalid). */
+/* Bytes of one page of one pool, of the workspace (0 if desc is invalid): 22 to 41 MB, for what the warps of an attention leave
+ * of rows that they share. */
 size_t gsi_kv_page_bytes(const gsi_kv_desc_t* desc);
 size_t gsi_kv_workspace_bytes(const gsi_kv_desc_t* desc);
 
