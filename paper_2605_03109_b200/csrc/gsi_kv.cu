@@ -324,13 +324,18 @@ __device__ __noinline__ uint32_t exact_codes(float4 x, float mid, float step, bo
 constexpr float kWhole = 12582912.f;   // 1.5 x 2^23: a sum with it is a whole number of its last digit
 
 // Codes of a lane's sixteen channels, four to 16 bits.  code - 8 = rint((x - mid) / s), where the product with 1 / s serves for
-// the quotient, a single fp32 division: it is off by 8.5 (2^-22 + 2^-24) at most, which only matters next to a border.
+// the quotient, a single fp32 division: it is off by 8.5 (2^-22 + 2^-24) at most, which only matters next to a border (where
+// 16-bit rows lie once in a thousand channels: their differences from mid often are a whole number and a half of steps).
 template <gsi_dtype_t kType>
 __device__ __forceinline__ void codes_of(const Quarters<kType>& q, const Scale& z, uint32_t (&got)[4]) {
   float far = 0.f;
+  auto exact = [&](int i) {
+    got[i] = exact_codes(make_float4(q.channel(4 * i), q.channel(4 * i + 1), q.channel(4 * i + 2), q.channel(4 * i + 3)), z.mid, z.step, z.finite);
+  };
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float v = 0.f;
+    if (kType != GSI_F32) far = 0.f;
 #pragma unroll
     for (int k = 3; k >= 0; --k) {
       const float r = __fsub_rn(q.channel(4 * i + k), z.mid) * z.inverse, whole = __fsub_rn(__fadd_rn(r, kWhole), kWhole);
@@ -338,11 +343,12 @@ __device__ __forceinline__ void codes_of(const Quarters<kType>& q, const Scale& 
       v = fmaf(v, 16.f, whole);
     }
     got[i] = __float_as_uint(v + (8388608.f + 0x8888)) & 0xFFFFu;   // (the sum of code 16^k, as a whole number)
+    if (kType != GSI_F32 && !(z.plain && far < 0.49999f)) exact(i);
   }
-  if (z.plain && far < 0.49999f) return;
+  if (kType == GSI_F32 && !(z.plain && far < 0.49999f)) {   // (seldom: one look for all)
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    got[i] = exact_codes(make_float4(q.channel(4 * i), q.channel(4 * i + 1), q.channel(4 * i + 2), q.channel(4 * i + 3)), z.mid, z.step, z.finite);
+    for (int i = 0; i < 4; ++i) exact(i);
+  }
 }
 
 // Of four lanes (quarters t of a row), each with four 16-bit pieces h[i] of piece group i: lane t gets group t's four, in
@@ -377,8 +383,8 @@ __device__ __forceinline__ unsigned char* block_of(const Shape& s, unsigned char
   return pages + tile_at(s, page, it.head, in / kTile) + it.group * kBlockBytes;
 }
 
-// K and V of a row are under way together.  Bound by issue for long prompts, 25 instructions a channel and lane: 16001 rows of 32 heads
-// of 128 take 125 us in bf16 (2.7 TB/s), 8000 in fp32 64 us (4.7 TB/s).
+// K and V of a row are under way together.  Bound by issue for long prompts (slots 75 % busy when all sixteen channels were divided): 16001 rows of 32 heads
+// of 128 take 106 us in bf16 (3.2 TB/s), 8000 in fp32 64 us (4.7 TB/s).
 template <gsi_dtype_t kType, bool kVec>
 __global__ void __launch_bounds__(kRowWarps * 32, kType == GSI_F32 ? 7 : 8) k_kv_append(Shape s, RowsArgs a, Control* ctl) {
   const int quarter = threadIdx.x & 3;
