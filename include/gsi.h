@@ -543,7 +543,7 @@ gsi_status_t gsi_kv_read(gsi_kv_t h, const void* pages, const int* slots, int n,
  *   out = sum_p softmax_p(scale q . k_p) v_p        0 where it sees none
  * q, out: n_rows rows of n_q_heads x head_dim of `dtype`, n_q_heads a multiple of n_heads: q head j goes with
  * head j / (n_q_heads / n_heads).  Strides in elements, channels adjacent, >= 0 (out's rows apart from each
- * other).  Rows behind the last sequence's are left as they were.  Softmax and sums are held in fp32; the contractions
+ * other, and from q's: columns of the same rows may hold both).  Rows behind the last sequence's are left as they were.  Softmax and sums are held in fp32; the contractions
  * take an fp32 q to 2^-24 of its row's largest channel and the probabilities in 22 bits, a 16-bit q as it is and the
  * probabilities in 11 bits.  A page number outside the
  * pool, or a length outside the table, is reported by the status word (GSI_ERR_INVALID_ARG) and gives

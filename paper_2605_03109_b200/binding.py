@@ -465,7 +465,7 @@ class KVCache:
 
     def attend(self, q: torch.Tensor, layer: int = 0, scale: float | None = None, out: torch.Tensor | None = None, stream=None):
         """Attention of the plan's rows, each over its request's tokens up to its own; ``scale`` is
-        ``head_dim ** -0.5`` by default.  Rows behind the last request's are not written."""
+        ``head_dim ** -0.5`` by default.  Rows behind the last request's are not written.  ``out`` shares no element with ``q``."""
         status, out = _calls.kv_attend(self._state, q, layer, self._scale if scale is None else scale, out, stream)
         if status:
             _check(status, "gsi_kv_attend")
