@@ -321,6 +321,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
   const int share = my_share + warp * stride;
 
   if (share < shares) {
+    __syncwarp();   // (what clear_rows wrote lies under other lanes' rows of q; votes and shuffles order no memory)
     const int mine = (int)(u1 - u0);   // the warp's units
     Seq q;
     int head = 0, row_tile = 0, unit = 0;   // of the next unit

@@ -799,3 +799,30 @@ def test_a_closed_cache_and_its_calls():
     c.close()
     with pytest.raises(g.GsiError):
         c.plan(ints([1]))
+
+
+def attend_of(c, q, n_seqs):
+    """The library's call with a number of requests of its own."""
+    from paper_2605_03109_b200 import binding
+    g, out = gsi(), torch.full_like(q, 9.0)
+    status = g.lib.gsi_kv_attend(c.handle, q.data_ptr(), {torch.float32: g.GSI_F32, torch.bfloat16: g.GSI_BF16}[q.dtype], q.stride(0), q.stride(1),
+                                 q.shape[0], q.shape[1], c.head_dim ** -0.5, c.q_start.data_ptr(), c.kv_len.data_ptr(), c.table.data_ptr(), n_seqs,
+                                 c.pages.data_ptr(), out.data_ptr(), out.stride(0), out.stride(1), binding._stream_ptr(None))
+    assert status == 0
+    return out
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_few_requests_and_many_are_shared_out_alike(dtype):
+    """Up to 32 requests a warp shares out by itself, more the block: empty ones behind them change nothing, call after call."""
+    rng = np.random.default_rng(31)
+    kv_len, news = [900, 17, 300, 1] + [0] * 36, [1, 1, 1, 1] + [0] * 36
+    c, table = a_cache(2, 128, 16, kv_len, news, rng)
+    kv = fill_and_read(c, rng, kv_len, table)
+    q = rows(rng, (6, 2, 128), dtype)
+    want = attend_of(c, q, 40)
+    check(c, q, want, torch.full_like(q, 9.0), kv, kv_len, news, 128 ** -0.5)
+    for _ in range(20):
+        for n in (4, 32, 33):
+            assert torch.equal(attend_of(c, q, n), want)
