@@ -41,7 +41,13 @@ constexpr int kGrid = 148;      // a block an SM (of two, the one that came firs
 constexpr int kFlush = 32;      // sets of tiles between sums in fp32 (T = 2)
 constexpr float kLow = 4096.f;  // units of the second term of q in one of the first
 constexpr float kLazy = 8.f;    // a running maximum is left where it is while 2^score stays below 2^kLazy above it
-constexpr float kOne = 64.f;    // p s <= 2^kLazy kOne s / vs < 2^15
+// p s enters as f16 terms: times kOne / (the largest p s so far, as a power of two), and anew where one passes kTop.  That is a
+// matter of a row and a block of channels: a step that is large in another block, or a token that the row does not see, or hardly,
+// takes no bits away.  Terms of 2^-30 of the largest p s are still held; below kLeast none is.
+constexpr float kOne = 64.f, kTop = 32768.f, kLeast = 0x1p-100f;
+// kOne / v of a power of two v in [kLeast, 2^100], and 1 / v
+__device__ __forceinline__ float over_power(float v) { return __uint_as_float((260u << 23) - __float_as_uint(v)); }
+__device__ __forceinline__ float inverse_power(float v) { return __uint_as_float((254u << 23) - __float_as_uint(v)); }
 constexpr float kNone = -3e38f; // the maximum of no score
 
 // G: blocks of 64 channels; T: f16 terms of an operand; NT: column tiles of eight; L: lane quarters of a tile.
@@ -549,7 +555,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
 
       // sums and maxima, of each tile of a unit its own until the segment ends
       float O[NT][G][4][4], z[NT][kLR][G], m[NT][kLR], l[NT][kLR], m_flush[NT], factor[NT][kLR];
-      float vs = 0.f, vinv = 0.f;   // a power of two not below any s of V so far, and kOne / vs
+      float unit_of[NT][kLR][G];   // of p s in O: kOne / (a power of two not below any p s so far); 0 before the first
       bool flushed = false;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -565,7 +571,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           l[n][r] = 0.f;
           factor[n][r] = s_factor[row_of(n, r)];
 #pragma unroll
-          for (int g = 0; g < G; ++g) z[n][r][g] = 0.f;
+          for (int g = 0; g < G; ++g) z[n][r][g] = unit_of[n][r][g] = 0.f;
         }
         m_flush[n] = kNone;
       }
@@ -633,24 +639,18 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
             return;
           }
         }
-        // pairs of V, and their largest step
-        uint2 pv[kSets][G];
-        __half2 steps = __half2half2(__ushort_as_half(0));
+        uint2 pv[kSets][G];   // pairs of V
 #pragma unroll
         for (int u = 0; u < kSets; ++u)
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
-            uint2& v = pv[u][g];
-            v = lds64(v_at + my_pair + (u * kSet * C::kStride + g * kBlockBytes));
-            if constexpr (kMasked) {   // (behind the last token lies anything)
-              const int at = pos + u * kSet * kTile;
-              if (wrong[u] || at >= q.len) v.x = 0u;
-              if (wrong[u] || at + 8 >= q.len) v.y = 0u;
-            }
-            steps = __hmax2(steps, __hmax2(*reinterpret_cast<const __half2*>(&v.x), *reinterpret_cast<const __half2*>(&v.y)));
-          }
-        const float step = __low2float(steps);
-        bool move = step > vs;
+          for (int g = 0; g < G; ++g) pv[u][g] = lds64(v_at + my_pair + (u * kSet * C::kStride + g * kBlockBytes));
+        // p s of token e; 0 for one that the row does not see (behind the last token lies anything)
+        auto weight_of = [&](int u, int n, int r, int g, int e) {
+          if (kMasked && sees(row_of(n, r)) - pos - u * kSet * kTile <= 8 * e) return 0.f;
+          return p[u][n][r][e] * __low2float(*reinterpret_cast<const __half2*>(e ? &pv[u][g].y : &pv[u][g].x));
+        };
+        float x[kSets][NT][kLR][G][2], top = 0.f;   // p s as it enters
+        bool move = false;
 #pragma unroll
         for (int u = 0; u < kSets; ++u)
 #pragma unroll
@@ -666,89 +666,100 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
               for (int e = 0; e < 2; ++e) {
                 p[u][n][r][e] = fmaf(S[u][n][r][e], kMasked ? 1.f : factor[n][r], -m[n][r]);
                 move = move || p[u][n][r][e] > kLazy;
+                p[u][n][r][e] = exp2_fast(p[u][n][r][e]);
               }
-            }
-        if (__any_sync(0xffffffffu, move)) {
-          float largest = step;
 #pragma unroll
-          for (int o = 4; o < 32; o <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
-          const float next_vs = fmaxf(vs, __uint_as_float((__float_as_uint(largest) + 0x7FFFFFu) & 0x7F800000u));
-          const float v_keep = next_vs > 0.f ? vs / next_vs : 1.f;
-          vs = next_vs;
-          vinv = vs > 0.f ? kOne / vs : 0.f;
-          float keep[NT][kLR];
+              for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  x[u][n][r][g][e] = weight_of(u, n, r, g, e) * unit_of[n][r][g];
+                  top = fmaxf(top, x[u][n][r][g][e]);
+                }
+            }
+        if (__any_sync(0xffffffffu, move || top > kTop)) {
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < kLR; ++r) {
               const float f = kMasked ? 1.f : factor[n][r];
-              float x = m[n][r];
+              float now = m[n][r];
 #pragma unroll
-              for (int u = 0; u < kSets; ++u) x = fmaxf(x, fmaxf(S[u][n][r][0] * f, S[u][n][r][1] * f));
+              for (int u = 0; u < kSets; ++u) now = fmaxf(now, fmaxf(S[u][n][r][0] * f, S[u][n][r][1] * f));
 #pragma unroll
-              for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-              if (x - m[n][r] <= kLazy) x = m[n][r];   // (another row's: this one's sums stay as they are)
-              keep[n][r] = exp2_fast(m[n][r] - x);
-              m[n][r] = x;
-              l[n][r] *= keep[n][r];
-#pragma unroll
-              for (int g = 0; g < G; ++g) z[n][r][g] *= keep[n][r];
-              keep[n][r] *= v_keep;
+              for (int o = 4; o < 32; o <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, o));
+              const bool moved = now - m[n][r] > kLazy;
+              if (!moved) now = m[n][r];   // (another row's: this one's sums stay as they are)
+              const float keep = exp2_fast(m[n][r] - now);
+              m[n][r] = now;
+              l[n][r] *= keep;
 #pragma unroll
               for (int u = 0; u < kSets; ++u)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) p[u][n][r][e] = fmaf(S[u][n][r][e], f, -x);
+                for (int e = 0; e < 2; ++e) p[u][n][r][e] = exp2_fast(fmaf(S[u][n][r][e], f, -now));
+#pragma unroll
+              for (int g = 0; g < G; ++g) {
+                z[n][r][g] *= keep;
+                float largest = 0.f;
+#pragma unroll
+                for (int u = 0; u < kSets; ++u)
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) {
+                    x[u][n][r][g][e] = weight_of(u, n, r, g, e);
+                    largest = fmaxf(largest, x[u][n][r][g][e]);
+                  }
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
+                float all = keep;   // what O is multiplied by
+                if (moved || largest * unit_of[n][r][g] > kTop) {
+                  const float was = unit_of[n][r][g] > 0.f ? over_power(unit_of[n][r][g]) : 0.f;
+                  const float next = __uint_as_float((__float_as_uint(fmaxf(fmaxf(was * keep, largest), kLeast)) + 0x7FFFFFu) & 0x7F800000u);
+                  all *= was * inverse_power(next);
+                  unit_of[n][r][g] = over_power(next);
+                }
+#pragma unroll
+                for (int u = 0; u < kSets; ++u)
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) x[u][n][r][g][e] *= unit_of[n][r][g];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    if (kLR == 1 || (e & 1) == r) O[n][g][i][e] *= all;
+              }
             }
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) O[n][g][i][e] *= keep[n][kLR == 2 ? e & 1 : 0];
         }
 #pragma unroll
         for (int u = 0; u < kSets; ++u) {
-        float ps[NT][kLR][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int r = 0; r < kLR; ++r)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              p[u][n][r][e] = exp2_fast(p[u][n][r][e]);
-              l[n][r] += p[u][n][r][e];
-              ps[n][r][e] = p[u][n][r][e] * vinv;
-            }
+            for (int e = 0; e < 2; ++e) l[n][r] += p[u][n][r][e];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          const float2 p0 = unpack_half2(pv[u][g].x), p1 = unpack_half2(pv[u][g].y);
+          const float mid0 = unpack_half2(pv[u][g].x).y, mid1 = unpack_half2(pv[u][g].y).y;
           uint32_t b0[NT], b1[NT];
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            float x[kLR][2];
 #pragma unroll
             for (int r = 0; r < kLR; ++r) {
-              x[r][0] = ps[n][r][0] * p0.x;
-              x[r][1] = ps[n][r][1] * p1.x;
               if constexpr (kMasked) {   // (a token that this row does not see need not be a number)
                 const int vis = sees(row_of(n, r)) - pos - u * kSet * kTile;
-                if (vis <= 0) x[r][0] = 0.f;
-                else z[n][r][g] = fmaf(p[u][n][r][0], p0.y, z[n][r][g]);
-                if (vis <= 8) x[r][1] = 0.f;
-                else z[n][r][g] = fmaf(p[u][n][r][1], p1.y, z[n][r][g]);
+                if (vis > 0) z[n][r][g] = fmaf(p[u][n][r][0], mid0, z[n][r][g]);
+                if (vis > 8) z[n][r][g] = fmaf(p[u][n][r][1], mid1, z[n][r][g]);
               } else {
-                z[n][r][g] = fmaf(p[u][n][r][1], p1.y, fmaf(p[u][n][r][0], p0.y, z[n][r][g]));
+                z[n][r][g] = fmaf(p[u][n][r][1], mid1, fmaf(p[u][n][r][0], mid0, z[n][r][g]));
               }
             }
             if constexpr (T == 2) {   // its upper eleven bits and the rest
-              const float h0 = __uint_as_float(__float_as_uint(x[0][0]) & 0xFFFFE000u), h1 = __uint_as_float(__float_as_uint(x[0][1]) & 0xFFFFE000u);
-              b0[n] = pack_half2(h0, x[0][0] - h0);
-              b1[n] = pack_half2(h1, x[0][1] - h1);
+              const float x0 = x[u][n][0][g][0], x1 = x[u][n][0][g][1];
+              const float h0 = __uint_as_float(__float_as_uint(x0) & 0xFFFFE000u), h1 = __uint_as_float(__float_as_uint(x1) & 0xFFFFE000u);
+              b0[n] = pack_half2(h0, x0 - h0);
+              b1[n] = pack_half2(h1, x1 - h1);
             } else {
-              b0[n] = pack_half2(x[0][0], x[kLR - 1][0]);
-              b1[n] = pack_half2(x[0][1], x[kLR - 1][1]);
+              b0[n] = pack_half2(x[u][n][0][g][0], x[u][n][kLR - 1][g][0]);
+              b1[n] = pack_half2(x[u][n][0][g][1], x[u][n][kLR - 1][g][1]);
             }
             b0[n] = transpose8x8(b0[n]);
             b1[n] = transpose8x8(b1[n]);
@@ -776,7 +787,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
       const bool tail = unit == 0;
       float* part = a.parts + (2ll * share + tail) * C::kPart;
       auto lane_sums = [&](int n, int g, int r, float (&v)[8]) {
-        const float f = vs * (1.f / kOne);
+        const float f = unit_of[n][r][g] > 0.f ? inverse_power(unit_of[n][r][g]) : 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           v[i] = (T == 2 ? O[n][g][i][0] + O[n][g][i][1] : O[n][g][i][r]) * f;

@@ -826,3 +826,66 @@ def test_few_requests_and_many_are_shared_out_alike(dtype):
     for _ in range(20):
         for n in (4, 32, 33):
             assert torch.equal(attend_of(c, q, n), want)
+
+
+def put(c, k, v, kv_len, table):
+    slots = slots_of(c, kv_len, table)
+    c.pages.fill_(0xFF)
+    c.append(k, v, slots=torch.from_numpy(slots).cuda())
+    return read_back(c, slots)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [2.0 ** 10, 2.0 ** 20, 2.0 ** -20])
+@pytest.mark.parametrize("dim,shared", [(128, 1), (128, 5), (256, 2)])
+def test_blocks_of_one_head_whose_values_differ_in_size(dtype, size, dim, shared):
+    """The block beside does not take bits away: each is within the bound of its own size."""
+    rng = np.random.default_rng(41)
+    kv_len, news = [150, 33], [1, 2]
+    c, table = a_cache(1, dim, 16, kv_len, news, rng)
+    k, v = (torch.from_numpy(rng.standard_normal((183, 1, dim)).astype(np.float32)).cuda() for _ in range(2))
+    v[..., 64:] *= size                              # (2^-20: steps that are subnormal in f16; 2^20: past its range)
+    kv = put(c, k, (v / 64 if size == 2.0 ** 20 else v), kv_len, table)
+    q = rows(rng, (3, shared, dim), dtype)
+    out = c.attend(q)
+    if dtype == torch.float16:                       # (values that fp16 does not hold are compared as they are held)
+        out = out.clamp(-65504, 65504)
+    check(c, q, out, out, kv, kv_len, news, dim ** -0.5)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("small,large", [(1.0, 3e4), (1e-3, 1e4), (1e-5, 1e2)])
+def test_a_token_that_is_not_seen_yet_takes_no_bits_away(dtype, small, large):
+    """Rows of a chunk beside a later token whose values are larger by far: the numbers of a call without that token's size."""
+    rng = np.random.default_rng(42)
+    kv_len, news = [70], [9]
+    c, table = a_cache(1, 128, 16, kv_len, news, rng)
+    k, v = (torch.from_numpy(rng.standard_normal((70, 1, 128)).astype(np.float32)).cuda() for _ in range(2))
+    v *= small
+    put(c, k, v, kv_len, table)
+    q = rows(rng, (9, 2, 128), dtype)
+    plain = c.attend(q)
+    v[69] *= large / small
+    kv = put(c, k, v, kv_len, table)
+    out = c.attend(q)
+    check(c, q, out, out, kv, kv_len, news, 128 ** -0.5)
+    assert torch.equal(out[:8], plain[:8])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("at", [0, 40, 99, 199])
+def test_a_large_value_with_a_small_probability(dtype, at):
+    """A token of a score far below the others' and of values far above them, seen first, in between and last."""
+    rng = np.random.default_rng(43 + at)
+    c, table = a_cache(1, 64, 16, [200], [1], rng)
+    k, v = (torch.from_numpy(rng.standard_normal((200, 1, 64)).astype(np.float32)).cuda() * w for w in (0.3, 3e-5))
+    k[:, 0, 5] = 0.0
+    k[at], v[at] = -40.0, v[at] * 3e8
+    kv = put(c, k, v, [200], table)
+    q = torch.zeros(1, 3, 64, dtype=dtype, device="cuda")
+    q[0, :, 5] = torch.tensor([1.0, 0.75, -0.125])   # e^-40, e^-30, and one that sees it as the largest of all
+    out = c.attend(q, scale=1.0)
+    check(c, q, out, out, kv, [200], [1], 1.0)
