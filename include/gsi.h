@@ -544,8 +544,9 @@ gsi_status_t gsi_kv_read(gsi_kv_t h, const void* pages, const int* slots, int n,
  * q, out: n_rows rows of n_q_heads x head_dim of `dtype`, n_q_heads a multiple of n_heads: q head j goes with
  * head j / (n_q_heads / n_heads).  Strides in elements, channels adjacent, >= 0 (out's rows apart from each
  * other, and from q's: columns of the same rows may hold both).  Rows behind the last sequence's are left as they were.  Softmax and sums are held in fp32; the contractions
- * take an fp32 q to 2^-24 of its row's largest channel and the probabilities in 22 bits, a 16-bit q as it is and the
- * probabilities in 11 bits.  A page number outside the
+ * take an fp32 q to 2^-24 of its row's largest channel, a 16-bit q as it is (to 2^-35 of that), and the probabilities, times the
+ * steps of v, in 22 bits (for each row and 64 channels, down to 2^-30 of the largest of them; with a bf16 q in 11 bits, an eighth of
+ * what the rounding of out takes).  A page number outside the
  * pool, or a length outside the table, is reported by the status word (GSI_ERR_INVALID_ARG) and gives
  * NaN in the rows that would see it.  Which sums are made where follows from the lengths; a call is reproducible
  * bit for bit.

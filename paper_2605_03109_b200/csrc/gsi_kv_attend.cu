@@ -17,7 +17,9 @@
 // = hi + lo / 4096 with |hi|, |lo| <= 2^11 (so q is held to 2^-24 of its row's largest): a block's sums of codes times
 // whole numbers stay below 2^21, and the tensor cores, which truncate as they add, add them exactly (with two f16 terms instead the
 // scores were three times as far off).  Those of p s are two f16 terms, 22 bits; their sums are handed over to
-// fp32 additions every kFlush sets of tiles.  16-bit rows take one column: q exact, p s in 11 bits.
+// fp32 additions every kFlush sets of tiles.  16-bit rows take one column: q exact (to 2^-35 of its row's largest).  p s of fp16 rows
+// are two terms, one after the other (with one, outputs of drafts were 2.8e-4 off instead of 2.1e-4; 42.5 -> 45 us); of bf16 rows one term, 11 bits,
+// 2^-12 where the output's own rounding takes 2^-9 (128 requests with shared heads: 1.67e-3 off with one, 1.66e-3 with two; 132 us against 148).
 //
 // Measured: one row of fp32, heads of 128, 240 warp instructions a tile (K and V of 16 tokens), issue slots 60 % and DRAM 94 % busy
 // once all warps run: 1.21 GB in 200 us, 6.0 TB/s.  A call has 6 us before its first tiles (lengths, shares, table, q) and
@@ -197,6 +199,8 @@ struct Pending {
 template <int G, int T, int L, int NT>
 __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Shape s, AttendArgs a, Control* ctl) {
   using C = Cfg<G, T, L, NT>;
+  constexpr int kTerms = 3 - T;   // of p s that follow one another, where a row has one column
+  const bool two = a.dtype == GSI_F16;          // both of them
   constexpr int kLR = C::kLaneRows, N = C::kTiles, kSet = C::kSet, kSets = C::kSets, kWarps = C::kWarps, kThreads = C::kThreads;
   static_assert(C::kRing >= (int)sizeof(Scan2) * kScan, "prefixes lie in the first warp's rings");
   extern __shared__ __align__(128) unsigned char smem[];
@@ -739,7 +743,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
 #pragma unroll
         for (int g = 0; g < G; ++g) {
           const float mid0 = unpack_half2(pv[u][g].x).y, mid1 = unpack_half2(pv[u][g].y).y;
-          uint32_t b0[NT], b1[NT];
+          uint32_t b0[NT][kTerms], b1[NT][kTerms];   // of tokens gr, of tokens gr + 8
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -752,17 +756,26 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
                 z[n][r][g] = fmaf(p[u][n][r][1], mid1, fmaf(p[u][n][r][0], mid0, z[n][r][g]));
               }
             }
-            if constexpr (T == 2) {   // its upper eleven bits and the rest
+            if constexpr (T == 2) {   // its upper eleven bits and the rest, side by side in the row's two columns
               const float x0 = x[u][n][0][g][0], x1 = x[u][n][0][g][1];
               const float h0 = __uint_as_float(__float_as_uint(x0) & 0xFFFFE000u), h1 = __uint_as_float(__float_as_uint(x1) & 0xFFFFE000u);
-              b0[n] = pack_half2(h0, x0 - h0);
-              b1[n] = pack_half2(h1, x1 - h1);
+              b0[n][0] = pack_half2(h0, x0 - h0);
+              b1[n][0] = pack_half2(h1, x1 - h1);
             } else {
-              b0[n] = pack_half2(x[u][n][0][g][0], x[u][n][kLR - 1][g][0]);
-              b1[n] = pack_half2(x[u][n][0][g][1], x[u][n][kLR - 1][g][1]);
+              auto term = [&](int e, uint32_t& first, uint32_t& second) {   // to nearest, and what is left
+                first = pack_half2(x[u][n][0][g][e], x[u][n][kLR - 1][g][e]);
+                const float2 high = unpack_half2(first);
+                if (two) second = pack_half2(x[u][n][0][g][e] - high.x, x[u][n][kLR - 1][g][e] - high.y);
+              };
+              term(0, b0[n][0], b0[n][kTerms - 1]);
+              term(1, b1[n][0], b1[n][kTerms - 1]);
             }
-            b0[n] = transpose8x8(b0[n]);
-            b1[n] = transpose8x8(b1[n]);
+#pragma unroll
+            for (int y = 0; y < kTerms; ++y) {
+              if (y && !two) continue;
+              b0[n][y] = transpose8x8(b0[n][y]);
+              b1[n][y] = transpose8x8(b1[n][y]);
+            }
           }
 #pragma unroll
           for (int i = 0; i < kSet; ++i) {
@@ -774,9 +787,13 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
                                       {centred<true>(x8), centred<true>(y8), centred<true>(z8), centred<true>(w8)}};
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              const uint32_t c0 = kSet == 1 ? b0[n] : b0[n] & only[i], c1 = kSet == 1 ? b1[n] : b1[n] & only[i];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) mma_f16(O[n][g][k], A[k][0], A[k][1], A[k][2], A[k][3], c0, c1);
+              for (int y = 0; y < kTerms; ++y) {
+                if (y && !two) continue;
+                const uint32_t c0 = kSet == 1 ? b0[n][y] : b0[n][y] & only[i], c1 = kSet == 1 ? b1[n][y] : b1[n][y] & only[i];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mma_f16(O[n][g][k], A[k][0], A[k][1], A[k][2], A[k][3], c0, c1);
+              }
             }
           }
         }

@@ -889,3 +889,27 @@ def test_a_large_value_with_a_small_probability(dtype, at):
     q[0, :, 5] = torch.tensor([1.0, 0.75, -0.125])   # e^-40, e^-30, and one that sees it as the largest of all
     out = c.attend(q, scale=1.0)
     check(c, q, out, out, kv, [200], [1], 1.0)
+
+
+@gpu
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+@pytest.mark.parametrize("shared,new", [(1, 1), (2, 1), (4, 1), (5, 5)])
+def test_probabilities_of_fp16_rows_have_22_bits(dim, shared, new):
+    """11 bits would show beside the outputs' own 11: within the bound of fp32 rows.  (Scores are small, so that their share of
+    the bound is; few tokens, so that roundings do not cancel.)"""
+    dtype = torch.float16
+    rng = np.random.default_rng(dim + shared)
+    kv_len, news, scale = [new, new + 1, 11, 40], [new] * 4, 1e-3
+    c, table = a_cache(1, dim, 16, kv_len, news, rng)
+    kv = fill_and_read(c, rng, kv_len, table)
+    q = rows(rng, (4 * new, shared, dim), dtype)
+    qn, got, half = q.float().cpu().numpy(), c.attend(q, scale=scale).double().cpu().numpy(), torch.finfo(dtype).eps / 2
+    first = 0
+    for i, n in enumerate(kv_len):
+        for m in range(new):
+            for h in range(shared):
+                have = [[x[first:first + n - new + m + 1, 0] for x in t] for t in kv]
+                want, off = R.attend(qn[i * new + m, h], *have, scale, False)
+                tol = off + half * np.abs(want) + 3e-8   # (half of f16's smallest step)
+                assert (np.abs(got[i * new + m, h] - want) <= tol).all(), (i, m, h)
+        first += n
