@@ -16,7 +16,7 @@
 // where sums of codes would cancel against the mid part.  fp32 rows take two columns each.  Those of q are whole numbers, q 2^k
 // = hi + lo / 4096 with |hi|, |lo| <= 2^11 (so q is held to 2^-24 of its row's largest): a block's sums of codes times
 // whole numbers stay below 2^21, and the tensor cores, which truncate as they add, add them exactly (with two f16 terms instead the
-// scores were three times as far off).  Those of p s are two f16 terms, 22 bits; their sums are handed over to
+// scores were three times as far off).  Those of p s are two f16 terms, 22 bits.  The sums of out are handed over to
 // fp32 additions every kFlush sets of tiles.  16-bit rows take one column: q exact (to 2^-35 of its row's largest).  p s of fp16 rows
 // are two terms, one after the other (with one, outputs of drafts were 2.8e-4 off instead of 2.1e-4; 42.5 -> 45 us); of bf16 rows one term, 11 bits,
 // 2^-12 where the output's own rounding takes 2^-9 (128 requests with shared heads: 1.67e-3 off with one, 1.66e-3 with two; 132 us against 148).
@@ -40,7 +40,6 @@ using umma::s32;
 
 constexpr int kScan = 256;      // threads that look through the sequences
 constexpr int kGrid = 148;      // a block an SM (of two, the one that came first ran ahead by an eighth)
-constexpr int kFlush = 32;      // sets of tiles between sums in fp32 (T = 2)
 constexpr float kLow = 4096.f;  // units of the second term of q in one of the first
 constexpr float kLazy = 8.f;    // a running maximum is left where it is while 2^score stays below 2^kLazy above it
 // p s enters as f16 terms: times kOne / (the largest p s so far, as a power of two), and anew where one passes kTop.  That is a
@@ -84,6 +83,9 @@ struct Cfg {
   static_assert(kShares <= kMaxShares, "the workspace's parts and tickets");
   static constexpr int kSnap = kTiles == 1 ? 2 : 1;        // units: the share of a warp ends with a segment that ends as near
   static constexpr int kCost = kSets == 2 ? 3 : L + 1;     // units that a segment itself counts as in a share (L: 111 us, L + 1: 109)
+  // Sets of tiles between sums in fp32, as the tensor cores truncate: 2^-23 of a sum each.  16-bit rows are rounded to 2^-12 or 2^-9 in
+  // the end (with 32 for them too: 128 requests with shared heads 136 -> 139 us).
+  static constexpr int kFlush = T == 2 ? 32 : 128;
   static constexpr int kPart = kPartFloats(G);
   static constexpr int kPartRows = kPart / (kDim + 8);
 };
@@ -468,7 +470,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
 
     // ---- segments of the share
     for (int j = 0; j < mine && !gave_up;) {
-      const int n_units = min(q.units - unit, mine - j);   // of this segment
+      const int n_units = min(q.units - unit, mine - j), begun = j, end = j + n_units;   // of this segment
       const int row0 = row_tile * C::kRows, n_rows = min(C::kRows, q.m * a.shared - row0);
       // row r of the tile: row of the step, q head; its tokens
       const int step0 = row0 / a.shared, in0 = row0 - step0 * a.shared;
@@ -558,9 +560,8 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
       }
 
       // sums and maxima, of each tile of a unit its own until the segment ends
-      float O[NT][G][4][4], z[NT][kLR][G], m[NT][kLR], l[NT][kLR], m_flush[NT], factor[NT][kLR];
+      float O[NT][G][4][4], z[NT][kLR][G], m[NT][kLR], l[NT][kLR], factor[NT][kLR];
       float unit_of[NT][kLR][G];   // of p s in O: kOne / (a power of two not below any p s so far); 0 before the first
-      bool flushed = false;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -577,7 +578,6 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
 #pragma unroll
           for (int g = 0; g < G; ++g) z[n][r][g] = unit_of[n][r][g] = 0.f;
         }
-        m_flush[n] = kNone;
       }
       const int least = sees(0), most = sees(n_rows - 1);
 
@@ -653,7 +653,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           if (kMasked && sees(row_of(n, r)) - pos - u * kSet * kTile <= 8 * e) return 0.f;
           return p[u][n][r][e] * __low2float(*reinterpret_cast<const __half2*>(e ? &pv[u][g].y : &pv[u][g].x));
         };
-        float x[kSets][NT][kLR][G][2], top = 0.f;   // p s as it enters
+        float top = 0.f;   // the largest p s, as it enters
         bool move = false;
 #pragma unroll
         for (int u = 0; u < kSets; ++u)
@@ -674,11 +674,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
               }
 #pragma unroll
               for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                  x[u][n][r][g][e] = weight_of(u, n, r, g, e) * unit_of[n][r][g];
-                  top = fmaxf(top, x[u][n][r][g][e]);
-                }
+                top = fmaxf(top, fmaxf(weight_of(u, n, r, g, 0), weight_of(u, n, r, g, 1)) * unit_of[n][r][g]);
             }
         if (__any_sync(0xffffffffu, move || top > kTop)) {
 #pragma unroll
@@ -707,10 +703,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
 #pragma unroll
                 for (int u = 0; u < kSets; ++u)
 #pragma unroll
-                  for (int e = 0; e < 2; ++e) {
-                    x[u][n][r][g][e] = weight_of(u, n, r, g, e);
-                    largest = fmaxf(largest, x[u][n][r][g][e]);
-                  }
+                  for (int e = 0; e < 2; ++e) largest = fmaxf(largest, weight_of(u, n, r, g, e));
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
                 float all = keep;   // what O is multiplied by
@@ -720,10 +713,6 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
                   all *= was * inverse_power(next);
                   unit_of[n][r][g] = over_power(next);
                 }
-#pragma unroll
-                for (int u = 0; u < kSets; ++u)
-#pragma unroll
-                  for (int e = 0; e < 2; ++e) x[u][n][r][g][e] *= unit_of[n][r][g];
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -746,8 +735,11 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           uint32_t b0[NT][kTerms], b1[NT][kTerms];   // of tokens gr, of tokens gr + 8
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
+            float x[kLR][2];   // p s as it enters
 #pragma unroll
             for (int r = 0; r < kLR; ++r) {
+              x[r][0] = weight_of(u, n, r, g, 0) * unit_of[n][r][g];
+              x[r][1] = weight_of(u, n, r, g, 1) * unit_of[n][r][g];
               if constexpr (kMasked) {   // (a token that this row does not see need not be a number)
                 const int vis = sees(row_of(n, r)) - pos - u * kSet * kTile;
                 if (vis > 0) z[n][r][g] = fmaf(p[u][n][r][0], mid0, z[n][r][g]);
@@ -757,15 +749,15 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
               }
             }
             if constexpr (T == 2) {   // its upper eleven bits and the rest, side by side in the row's two columns
-              const float x0 = x[u][n][0][g][0], x1 = x[u][n][0][g][1];
+              const float x0 = x[0][0], x1 = x[0][1];
               const float h0 = __uint_as_float(__float_as_uint(x0) & 0xFFFFE000u), h1 = __uint_as_float(__float_as_uint(x1) & 0xFFFFE000u);
               b0[n][0] = pack_half2(h0, x0 - h0);
               b1[n][0] = pack_half2(h1, x1 - h1);
             } else {
               auto term = [&](int e, uint32_t& first, uint32_t& second) {   // to nearest, and what is left
-                first = pack_half2(x[u][n][0][g][e], x[u][n][kLR - 1][g][e]);
+                first = pack_half2(x[0][e], x[kLR - 1][e]);
                 const float2 high = unpack_half2(first);
-                if (two) second = pack_half2(x[u][n][0][g][e] - high.x, x[u][n][kLR - 1][g][e] - high.y);
+                if (two) second = pack_half2(x[0][e] - high.x, x[kLR - 1][e] - high.y);
               };
               term(0, b0[n][0], b0[n][kTerms - 1]);
               term(1, b1[n][0], b1[n][kTerms - 1]);
@@ -803,6 +795,8 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
       // the warp's part of a segment that it shares (or that it has to sum in pieces): channels 8 gr .. + 7 of a block
       const bool tail = unit == 0;
       float* part = a.parts + (2ll * share + tail) * C::kPart;
+      auto flush_row = [&](int n, int r) { return (n * 4 + t4) * kLR + r; };   // (the one that the row's sums go to in the end, where the lane has it)
+      auto maximum_at = [&](int n, int r) { return part + C::kPartRows * (C::kDim + 2) + flush_row(n, r); };   // that they were flushed at
       auto lane_sums = [&](int n, int g, int r, float (&v)[8]) {
         const float f = unit_of[n][r][g] > 0.f ? inverse_power(unit_of[n][r][g]) : 0.f;
 #pragma unroll
@@ -810,9 +804,9 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           v[i] = (T == 2 ? O[n][g][i][0] + O[n][g][i][1] : O[n][g][i][r]) * f;
           v[i + 4] = (T == 2 ? O[n][g][i][2] + O[n][g][i][3] : O[n][g][i][2 + r]) * f;
         }
-        if (T == 2 && flushed) {
-          const float keep = exp2_fast(m_flush[n] - m[n][r]);
-          const float4* from = reinterpret_cast<const float4*>(part + (n * 4 + t4) * C::kDim + g * kGroup + gr * 8);
+        if ((j - begun) * kSets > C::kFlush) {   // (not the first)
+          const float keep = exp2_fast(__ldcg(maximum_at(n, r)) - m[n][r]);
+          const float4* from = reinterpret_cast<const float4*>(part + flush_row(n, r) * C::kDim + g * kGroup + gr * 8);
           const float4 x = __ldcg(from), y = __ldcg(from + 1);
           v[0] = fmaf(x.x, keep, v[0]), v[1] = fmaf(x.y, keep, v[1]), v[2] = fmaf(x.z, keep, v[2]), v[3] = fmaf(x.w, keep, v[3]);
           v[4] = fmaf(y.x, keep, v[4]), v[5] = fmaf(y.y, keep, v[5]), v[6] = fmaf(y.z, keep, v[6]), v[7] = fmaf(y.w, keep, v[7]);
@@ -824,8 +818,6 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
         __stcg(to + 1, make_float4(v[4], v[5], v[6], v[7]));
       };
 
-      const int end = j + n_units;
-      int since = 0;
       for (int pos = unit * N * kTile; j < end; pos += N * kTile) {
         if (__any_sync(0xffffffffu, !mbar_wait(bars + stage, phase))) gave_up = true;
         if (gave_up) break;
@@ -848,23 +840,25 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           phase ^= 1u;
         }
         ++j;
-        if (T == 2 && (since += kSets) >= kFlush && j < end) {
-          since = 0;
+        if ((j - begun) * kSets % C::kFlush == 0 && j < end) {
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-              float v[8];
-              lane_sums(n, g, 0, v);
-              to_part(n * 4 + t4, g, v);
+#pragma unroll
+              for (int r = 0; r < kLR; ++r) {
+                float v[8];
+                lane_sums(n, g, r, v);
+                to_part(flush_row(n, r), g, v);
+              }
 #pragma unroll
               for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) O[n][g][i][e] = 0.f;
             }
-            m_flush[n] = m[n][0];
+#pragma unroll
+            for (int r = 0; r < kLR; ++r) __stcg(maximum_at(n, r), m[n][r]);   // (by each lane that reads it)
           }
-          flushed = true;
         }
       }
       if (gave_up) {
@@ -1070,7 +1064,7 @@ template <int G, int T, int L, int NT>
 cudaError_t launch(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
   using C = Cfg<G, T, L, NT>;
   static_assert(C::kSmem + 6144 <= 232448, "with what else a block holds in shared memory");
-  static_assert(C::kRows <= C::kPartRows && 4 * NT <= C::kPartRows && C::kHalf % 16 == 0 && C::kStages >= 1, "layout");
+  static_assert(C::kRows <= C::kPartRows && 4 * NT * C::kLaneRows <= C::kPartRows && C::kHalf % 16 == 0 && C::kStages >= 1, "layout");
   if (!a.q) return cudaFuncSetAttribute(k_kv_attend<G, T, L, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   return launch_pdl(k_kv_attend<G, T, L, NT>, dim3(kGrid), dim3(C::kThreads), C::kSmem, stream, s, a, ctl);
 }

@@ -111,8 +111,8 @@ def attend(q, k, v, scale, sixteen):
       roundings of the scaling; the sizes are those of q x (code s) and of the offset mid - 8 s;
       probabilities: e^x is off by 2^-22 and by the rounding of its argument, 3 x 2^-24 |score|; the rounding to the
       operand, u, and 2^-24 for the product with s;
-      the output: 16 instructions between sums in fp32, then a sum of up to 8 warps and the CTAs: 40 steps of 2^-23 of the
-      sum of the terms' sizes."""
+      the output: up to 32 (128) instructions between sums in fp32, and 40 steps of 2^-23 of the sum of the terms' sizes in all.  That is
+      less than the worst that can come of long shares, where each lane adds hundreds of terms in fp32: attend_of_long_shares."""
     u = 2.0 ** -12 if sixteen else 2.0 ** -23
     kv, ks, vs = [], [], []
     for codes, s, mid in (k, v):
@@ -132,3 +132,18 @@ def attend(q, k, v, scale, sixteen):
     p = p / total
     rel = 2 * off.max() + 2 * (2.0 ** -22 + 3 * 2.0 ** -24 * np.abs(score).max() * 2) + u + 2.0 ** -23 + 40 * 2.0 ** -23
     return p @ kv[1], (p[:, None] * vs[1]).sum(0) * rel
+
+
+def attend_of_long_shares(q, k, v, scale, sixteen, sets, parts):
+    """attend() where warps have up to `sets` sets of tiles each, and a row's sums come of `parts` of them.  Beside the 32 truncated
+    additions between sums in fp32 (128 of 16-bit rows), a lane adds two tokens a set to the sum of the probabilities and two to the mid part, and a flushed
+    sum every 32 sets; then come its 32 lanes (5 additions) and the parts: 2^-24 of the sum of the terms' sizes each, and e^x between the
+    flushed sums, the parts and the rest, 2^-22."""
+    want, off = attend(q, k, v, scale, sixteen)
+    (kc, kscale, kmid), (_, s, mid) = k, v
+    D = kc.shape[-1]
+    wide = lambda x: np.repeat(x.astype(np.float64), 64, -1)[..., :D]  # noqa: E731
+    score = (wide(kscale) * (kc.astype(np.float64) - 8) + wide(kmid)) @ q.astype(np.float64) * scale
+    p = np.exp(score - score.max())
+    sizes = (p / p.sum()) @ (8 * wide(s) + np.abs(wide(mid)))
+    return want, off + sizes * ((4 * sets + sets // 32 + 2 * 5 + 2 * parts) * 2.0 ** -24 + 2 * 2.0 ** -22 + (96 * 2.0 ** -23 if sixteen else 0))

@@ -913,3 +913,33 @@ def test_probabilities_of_fp16_rows_have_22_bits(dim, shared, new):
                 tol = off + half * np.abs(want) + 3e-8   # (half of f16's smallest step)
                 assert (np.abs(got[i * new + m, h] - want) <= tol).all(), (i, m, h)
         first += n
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dim,heads,seqs,new,length", [(64, 128, 3, 1, 160007), (128, 16, 3, 1, 160007), (64, 32, 2, 4, 120011), (256, 16, 4, 1, 100003), (64, 16, 2, 16, 60001)])
+def test_hundreds_of_sets_of_tiles_a_warp(dtype, dim, heads, seqs, new, length):
+    """Long requests (their tables name the same pages again and again): sums are handed over many times, of every type of row."""
+    rng = np.random.default_rng(dim + new)
+    g, page, n_pages = gsi(), 64, 37
+    c = g.KVCache(heads, dim, n_pages, seqs, length, page_tokens=page, max_tokens=seqs * new)
+    fill(c, rng, [n_pages * page], np.arange(n_pages)[None])
+    lens, news = [length - 1000 * i for i in range(seqs)], [new] * seqs
+    table = rng.integers(0, n_pages, tuple(c.table.shape))
+    c.table.copy_(torch.from_numpy(table))
+    c.kv_len.copy_(ints(lens))
+    c.q_start.copy_(ints([new * i for i in range(seqs + 1)]))
+    q = rows(rng, (seqs * new, heads, dim), dtype)
+    out = c.attend(q)
+    assert torch.equal(c.attend(q), out) and c.status() == 0
+    qn, got, half = q.float().cpu().numpy(), out.double().cpu().numpy(), torch.finfo(dtype).eps / 2
+    pool = c.pages.view(-1).cpu().numpy()
+    tiles = sum(-(-n // 16) for n in lens) * heads * -(-new // 4)       # (of a set or less each; at least four rows a unit but for single ones)
+    sets, parts = -(-tiles // (148 * 12)) + 8, -(-2400 // (seqs * heads)) + 2
+    for i, h in ((0, 0), (seqs - 1, heads - 1), (seqs // 2, heads // 3)):
+        k, v = R.decode(pool, (heads, dim, page), slots_of(c, [lens[i]], table[i:i + 1]), [h])
+        for m in sorted({0, new - 1}):
+            sees = lens[i] - new + m + 1
+            want, off = R.attend_of_long_shares(qn[i * new + m, h], *[[y[:sees, 0] for y in z] for z in (k, v)], dim ** -0.5, dtype != torch.float32, sets, parts)
+            tol = off + half * np.abs(want) + (3e-8 if dtype == torch.float16 else 0)
+            assert (np.abs(got[i * new + m, h] - want) <= tol).all(), (i, h, m, float((np.abs(got[i * new + m, h] - want) / tol).max()))
