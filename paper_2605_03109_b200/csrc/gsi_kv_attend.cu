@@ -18,8 +18,8 @@
 // whole numbers stay below 2^21, and the tensor cores, which truncate as they add, add them exactly (with two f16 terms instead the
 // scores were three times as far off).  Those of p s are two f16 terms, 22 bits.  The sums of out are handed over to
 // fp32 additions every kFlush sets of tiles.  16-bit rows take one column: q exact (to 2^-35 of its row's largest).  p s of fp16 rows
-// are two terms, one after the other (with one, outputs of drafts were 2.8e-4 off instead of 2.1e-4; 42.5 -> 45 us); of bf16 rows one term, 11 bits,
-// 2^-12 where the output's own rounding takes 2^-9 (128 requests with shared heads: 1.67e-3 off with one, 1.66e-3 with two; 132 us against 148).
+// are two terms, one after the other (with one, outputs of drafts were 2.8e-4 off instead of 2.1e-4); of bf16 rows one term, 11 bits,
+// 2^-12 where the output's own rounding takes 2^-9 (128 requests with shared heads: 1.67e-3 off with one, 1.66e-3 with two; 135 us against 146).
 //
 // Measured: one row of fp32, heads of 128, 240 warp instructions a tile (K and V of 16 tokens), issue slots 60 % and DRAM 94 % busy
 // once all warps run: 1.21 GB in 200 us, 6.0 TB/s.  A call has 6 us before its first tiles (lengths, shares, table, q) and
@@ -56,11 +56,15 @@ constexpr float kNone = -3e38f; // the maximum of no score
 // (rows t % L, T = 2; 2 (t % L) and the next, T = 1).  Few rows so share the scalar work of a tile's scores, where they would
 // leave most columns empty (one row: 188 -> 160 us for the 64 requests above).  A unit of work is one such set of tiles (two, where
 // a set is one tile and the registers have room: chunks of prompts 60 -> 54 us) of one head and a tile of rows.
+// A kernel for each type: with fp16 and bf16 told apart at run time 64 requests of bf16 rows, 32 heads of 128, took 129 us instead of 115.
+template <gsi_dtype_t kType>
+constexpr int kColumns = kType == GSI_F32 ? 2 : 1;
 template <int G, int T, int L, int NT>
 struct Cfg {
-  // Twelve warps where sixteen would leave too few registers: what is spilled comes back behind the tiles in flight (one request
-  // of 32771 tokens, 16 heads of 256: 52 us with sixteen, 49 with twelve).
-  static constexpr int kWarps = G >= 3 || G * NT == 4 ? 12 : 16;
+  // Twelve warps where sixteen would spill by the hundred bytes within the loop; what is spilled comes back behind the tiles in flight
+  // (one request of 32771 tokens, 16 heads of 256: 52 us with sixteen, 49 with twelve; drafts of 5 fp16 rows 46.8 and 40.3; 64 requests, 8 x 2 heads
+  // of 128, bf16: 48.5 and 43.3; chunks of fp32 rows, heads of 64: 50.4 and 50.3).  Heads of 128 with sixteen 16-bit rows still spill 192.
+  static constexpr int kWarps = G >= 3 || (L == 4 && G * NT >= 2) || (T == 1 && G == 2) ? 12 : 16;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kShares = kGrid * kWarps;
   static constexpr int kDim = G * kGroup;
@@ -198,11 +202,11 @@ struct Pending {
   long long out[kMaxRows];
 };
 
-template <int G, int T, int L, int NT>
-__global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Shape s, AttendArgs a, Control* ctl) {
+template <int G, gsi_dtype_t kType, int L, int NT>
+__global__ void __launch_bounds__(Cfg<G, kColumns<kType>, L, NT>::kThreads, 1) k_kv_attend(Shape s, AttendArgs a, Control* ctl) {
+  constexpr int T = kColumns<kType>;
   using C = Cfg<G, T, L, NT>;
-  constexpr int kTerms = 3 - T;   // of p s that follow one another, where a row has one column
-  const bool two = a.dtype == GSI_F16;          // both of them
+  constexpr int kTerms = kType == GSI_F16 ? 2 : 1;   // of p s that follow one another, where a row has one column
   constexpr int kLR = C::kLaneRows, N = C::kTiles, kSet = C::kSet, kSets = C::kSets, kWarps = C::kWarps, kThreads = C::kThreads;
   static_assert(C::kRing >= (int)sizeof(Scan2) * kScan, "prefixes lie in the first warp's rings");
   extern __shared__ __align__(128) unsigned char smem[];
@@ -381,7 +385,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
     auto channel = [&](int i) {
       if (T == 2) return __uint_as_float(q_raw[i]);
       const uint32_t w = q_raw[i / 2 % (T == 2 ? 8 : 4)];
-      if (a.dtype == GSI_BF16) return __uint_as_float((i & 1) ? w & 0xFFFF0000u : w << 16);
+      if (kType == GSI_BF16) return __uint_as_float((i & 1) ? w & 0xFFFF0000u : w << 16);
       return __half2float(__ushort_as_half((unsigned short)(w >> 16 * (i & 1))));
     };
     // row r of a tile of rows, from the step's row `step0` and the q head `in0` of those that share the head on
@@ -757,14 +761,13 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
               auto term = [&](int e, uint32_t& first, uint32_t& second) {   // to nearest, and what is left
                 first = pack_half2(x[0][e], x[kLR - 1][e]);
                 const float2 high = unpack_half2(first);
-                if (two) second = pack_half2(x[0][e] - high.x, x[kLR - 1][e] - high.y);
+                if (kTerms == 2) second = pack_half2(x[0][e] - high.x, x[kLR - 1][e] - high.y);
               };
               term(0, b0[n][0], b0[n][kTerms - 1]);
               term(1, b1[n][0], b1[n][kTerms - 1]);
             }
 #pragma unroll
             for (int y = 0; y < kTerms; ++y) {
-              if (y && !two) continue;
               b0[n][y] = transpose8x8(b0[n][y]);
               b1[n][y] = transpose8x8(b1[n][y]);
             }
@@ -781,7 +784,6 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
             for (int n = 0; n < NT; ++n) {
 #pragma unroll
               for (int y = 0; y < kTerms; ++y) {
-                if (y && !two) continue;
                 const uint32_t c0 = kSet == 1 ? b0[n][y] : b0[n][y] & only[i], c1 = kSet == 1 ? b1[n][y] : b1[n][y] & only[i];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) mma_f16(O[n][g][k], A[k][0], A[k][1], A[k][2], A[k][3], c0, c1);
@@ -903,7 +905,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 const int c = g * kGroup + gr * 8 + i;
-                if (c < s.head_dim) store_from_float(a.out, a.dtype, to + c, v[i] * over);
+                if (c < s.head_dim) store_from_float(a.out, kType, to + c, v[i] * over);
               }
             } else {
               to_part(row, g, v);
@@ -954,7 +956,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
             }
             const long long to = (long long)(q.q0 + step_row(r)) * a.out_token + q_head(r) * a.out_head + c4 * 4;
             for (int e = 0; e < 4; ++e)
-              if (c4 * 4 + e < s.head_dim) store_from_float(a.out, a.dtype, to + e, all == 0.f ? 0.f : v[e] / all);
+              if (c4 * 4 + e < s.head_dim) store_from_float(a.out, kType, to + e, all == 0.f ? 0.f : v[e] / all);
           }
         } else if (last && lane == 0) {
           Pending& x = s_pending[atomicAdd(&s_n_pending, 1)];
@@ -1052,7 +1054,7 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
           const float all = s_all[r], sums[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if (c4 * 4 + k < s.head_dim) store_from_float(a.out, a.dtype, x.out[r0 + r] + c4 * 4 + k, all == 0.f ? 0.f : sums[k] / all);
+            if (c4 * 4 + k < s.head_dim) store_from_float(a.out, kType, x.out[r0 + r] + c4 * 4 + k, all == 0.f ? 0.f : sums[k] / all);
         }
       }
       __syncthreads();
@@ -1060,56 +1062,57 @@ __global__ void __launch_bounds__(Cfg<G, T, L, NT>::kThreads, 1) k_kv_attend(Sha
   }
 }
 
-template <int G, int T, int L, int NT>
+template <int G, gsi_dtype_t kType, int L, int NT>
 cudaError_t launch(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
-  using C = Cfg<G, T, L, NT>;
+  using C = Cfg<G, kColumns<kType>, L, NT>;
   static_assert(C::kSmem + 6144 <= 232448, "with what else a block holds in shared memory");
   static_assert(C::kRows <= C::kPartRows && 4 * NT * C::kLaneRows <= C::kPartRows && C::kHalf % 16 == 0 && C::kStages >= 1, "layout");
-  if (!a.q) return cudaFuncSetAttribute(k_kv_attend<G, T, L, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
-  return launch_pdl(k_kv_attend<G, T, L, NT>, dim3(kGrid), dim3(C::kThreads), C::kSmem, stream, s, a, ctl);
+  if (!a.q) return cudaFuncSetAttribute(k_kv_attend<G, kType, L, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  return launch_pdl(k_kv_attend<G, kType, L, NT>, dim3(kGrid), dim3(C::kThreads), C::kSmem, stream, s, a, ctl);
 }
 
 // `rows`: of a unit, in column pairs (1, 2, 4, or 8 in two column tiles)
-template <int G, int T>
+template <int G, gsi_dtype_t kType>
 cudaError_t launch_rows(int rows, const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
   if constexpr (G <= 2) {
-    if (rows == 1) return launch<G, T, 1, 1>(s, a, ctl, stream);
-    if (rows == 8) return launch<G, T, 4, 2>(s, a, ctl, stream);
+    if (rows == 1) return launch<G, kType, 1, 1>(s, a, ctl, stream);
+    if (rows == 8) return launch<G, kType, 4, 2>(s, a, ctl, stream);
   }
-  if (rows <= 2) return launch<G, T, 2, 1>(s, a, ctl, stream);
-  return launch<G, T, 4, 1>(s, a, ctl, stream);
+  if (rows <= 2) return launch<G, kType, 2, 1>(s, a, ctl, stream);
+  return launch<G, kType, 4, 1>(s, a, ctl, stream);
 }
-cudaError_t launch_any(bool two, int rows, const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
-  switch (s.groups * 2 + two) {
-    case 2: return launch_rows<1, 1>(rows, s, a, ctl, stream);
-    case 3: return launch_rows<1, 2>(rows, s, a, ctl, stream);
-    case 4: return launch_rows<2, 1>(rows, s, a, ctl, stream);
-    case 5: return launch_rows<2, 2>(rows, s, a, ctl, stream);
-    case 6: return launch_rows<3, 1>(rows, s, a, ctl, stream);
-    case 7: return launch_rows<3, 2>(rows, s, a, ctl, stream);
-    case 8: return launch_rows<4, 1>(rows, s, a, ctl, stream);
-    default: return launch_rows<4, 2>(rows, s, a, ctl, stream);
+template <gsi_dtype_t kType>
+cudaError_t launch_groups(int rows, const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
+  switch (s.groups) {
+    case 1: return launch_rows<1, kType>(rows, s, a, ctl, stream);
+    case 2: return launch_rows<2, kType>(rows, s, a, ctl, stream);
+    case 3: return launch_rows<3, kType>(rows, s, a, ctl, stream);
+    default: return launch_rows<4, kType>(rows, s, a, ctl, stream);
   }
+}
+cudaError_t launch_any(gsi_dtype_t type, int rows, const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
+  return type == GSI_F32 ? launch_groups<GSI_F32>(rows, s, a, ctl, stream) : type == GSI_BF16 ? launch_groups<GSI_BF16>(rows, s, a, ctl, stream)
+                                                                                           : launch_groups<GSI_F16>(rows, s, a, ctl, stream);
 }
 
 }  // namespace
 
 cudaError_t prepare_attend(const Shape& s) {
-  for (int i = 0; i < 8; ++i) {
-    const cudaError_t e = launch_any(i & 1, 1 << i / 2, s, AttendArgs{}, nullptr, nullptr);
-    if (e != cudaSuccess) return e;
-  }
+  for (const gsi_dtype_t type : {GSI_F32, GSI_BF16, GSI_F16})
+    for (int rows = 1; rows <= 8; rows *= 2) {
+      const cudaError_t e = launch_any(type, rows, s, AttendArgs{}, nullptr, nullptr);
+      if (e != cudaSuccess) return e;
+    }
   return cudaSuccess;
 }
 
 cudaError_t launch_attend(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
   // The smallest unit that holds the rows of a sequence on average (half a row left over may go to a second tile of rows:
   // batches are padded).
-  const bool two = a.dtype == GSI_F32;
   const double mean = (double)a.n_rows * a.shared / a.n_seqs - 0.5;
   int rows = 1;
-  while (rows < 8 && rows * (two ? 1 : 2) < mean) rows *= 2;
-  return launch_any(two, rows, s, a, ctl, stream);
+  while (rows < 8 && rows * (a.dtype == GSI_F32 ? 1 : 2) < mean) rows *= 2;
+  return launch_any(a.dtype, rows, s, a, ctl, stream);
 }
 
 }  // namespace kv
