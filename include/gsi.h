@@ -474,6 +474,11 @@ gsi_status_t gsi_stack_destroy(gsi_stack_t s);
 #define GSI_KV_MAX_HEADS 8192
 #define GSI_KV_MAX_DIM 256
 
+enum {
+  GSI_KV_COMMIT = 1,  /* gsi_kv_plan: lens and *n_free move on                     */
+  GSI_KV_ALL_SEQS = 2 /* gsi_kv_plan: q_start and kv_len are written to their ends */
+};
+
 typedef struct {
   int n_heads;     /* heads of K and V, 1..GSI_KV_MAX_HEADS                         */
   int head_dim;    /* channels of a head, 1..GSI_KV_MAX_DIM                         */
@@ -511,8 +516,10 @@ gsi_status_t gsi_kv_create(const gsi_kv_desc_t* desc, void* workspace, size_t wo
  * Refused, and left as it was, is a sequence that needs a page where the pages asked for up to and with it
  * are more than the free ones (those behind it that need none are served), one that would be longer than its
  * table's row, one whose rows end behind max_tokens, one with n_new < 0 (which counts as no rows).
- * commit = 1: lens and *n_free move on.  commit = 0: they stay, so the next plan hands out the same pages
- * again (a step that may be taken back).  One launch.
+ * commit & GSI_KV_COMMIT: lens and *n_free move on.  Without it they stay, so the next plan hands out the same pages
+ * again (a step that may be taken back).  commit & GSI_KV_ALL_SEQS: q_start has max_seqs + 1 elements and kv_len max_seqs, and
+ * requests from n_seqs on get no rows and no tokens, so that an attention over max_seqs requests goes by whichever plan
+ * ran last, in a replayed graph too.  One launch.
  */
 gsi_status_t gsi_kv_plan(gsi_kv_t h, const int* n_new, int n_seqs, int commit, int* lens, int* n_free,
                          const int* free_pages, int* table, int* q_start, int* kv_len, int* slots,
@@ -548,8 +555,8 @@ gsi_status_t gsi_kv_read(gsi_kv_t h, const void* pages, const int* slots, int n,
  * steps of v, in 22 bits (for each row and 64 channels, down to 2^-30 of the largest of them; with a bf16 q in 11 bits, an eighth of
  * what the rounding of out takes).  A page number outside the
  * pool, or a length outside the table, is reported by the status word (GSI_ERR_INVALID_ARG) and gives
- * NaN in the rows that would see it.  Which sums are made where follows from the lengths; a call is reproducible
- * bit for bit.
+ * NaN in the rows that would see it.  Which sums are made where follows from the lengths, n_rows, n_seqs and the number
+ * of requests of the handle's last gsi_kv_plan call, by which a form for few or many rows is taken; a call is reproducible bit for bit.
  */
 gsi_status_t gsi_kv_attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t q_token_stride,
                            int64_t q_head_stride, int n_rows, int n_q_heads, float scale, const int* q_start,

@@ -402,7 +402,8 @@ class KVCache:
     Device tensors: the state ``lens``, ``table``, ``free``, ``n_free``, and what a plan leaves, ``q_start``,
     ``kv_len``, ``slots``, ``positions``, ``counts`` (new tokens, pages taken, pages left, requests refused).  None is
     read on the host, so a step can be captured into a CUDA graph.  ``pages`` (uint8, [n_layers][n_pages][bytes of a
-    page]) may be the caller's memory.  One cache may be used by one stream at a time.
+    page]) may be the caller's memory.  A plan may be for the first few requests only; those behind have no rows then.  One cache may be used
+    by one stream at a time.
     """
 
     def __init__(self, n_heads: int, head_dim: int, n_pages: int, max_seqs: int, max_len: int, page_tokens: int = 64,

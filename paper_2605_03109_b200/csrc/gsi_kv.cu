@@ -105,9 +105,13 @@ __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, C
   }
   if (took) atomicMax(&s_took, took);   // (the largest that is served: one result in any order)
   if (refused) atomicAdd(&s_refused, refused);
+  if (blockIdx.x == 0)   // (requests that the plan is not about have no rows)
+    for (int i = a.n_seqs + threadIdx.x; i <= a.upto; i += threads) {
+      a.q_start[i] = clamp_int(n_rows);
+      if (i < a.upto) a.kv_len[i] = 0;
+    }
   __syncthreads();
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    a.q_start[a.n_seqs] = clamp_int(n_rows);
     a.counts[0] = clamp_int(n_rows);
     a.counts[1] = s_took;
     a.counts[2] = n_free - s_took;
@@ -580,6 +584,7 @@ struct gsi_kv {
   float* parts;
   unsigned* tickets;
   int device;
+  int planned;   // requests of the last plan
   cudaStream_t last_stream;
 };
 
@@ -669,6 +674,7 @@ gsi_status_t gsi_kv_create(const gsi_kv_desc_t* desc, void* workspace, size_t wo
   h->ctl = reinterpret_cast<kv::Control*>(ws);
   h->tickets = reinterpret_cast<unsigned*>(ws + up256(sizeof(kv::Control)));
   h->parts = reinterpret_cast<float*>(ws + up256(sizeof(kv::Control)) + up256(kv::kMaxShares * 4));
+  h->planned = 0;
   h->last_stream = stream;
   if (cudaGetDevice(&h->device) != cudaSuccess || kv::prepare_attend(s) != cudaSuccess ||
       cudaMemsetAsync(ws, 0, up256(sizeof(kv::Control)) + up256(kv::kMaxShares * 4), stream) != cudaSuccess ||
@@ -682,14 +688,15 @@ gsi_status_t gsi_kv_create(const gsi_kv_desc_t* desc, void* workspace, size_t wo
 
 gsi_status_t gsi_kv_plan(gsi_kv_t h, const int* n_new, int n_seqs, int commit, int* lens, int* n_free, const int* free_pages, int* table,
                          int* q_start, int* kv_len, int* slots, int* positions, int* counts, gsi_stream_t stream) {
-  if (!h || n_seqs <= 0 || n_seqs > h->shape.max_seqs || (commit != 0 && commit != 1)) return GSI_ERR_INVALID_ARG;
+  if (!h || n_seqs <= 0 || n_seqs > h->shape.max_seqs || (commit & ~(GSI_KV_COMMIT | GSI_KV_ALL_SEQS))) return GSI_ERR_INVALID_ARG;
   for (const void* p : {(const void*)n_new, (const void*)lens, (const void*)n_free, (const void*)free_pages, (const void*)table,
                         (const void*)q_start, (const void*)kv_len, (const void*)slots, (const void*)positions, (const void*)counts})
     if (!aligned(p, 4)) return GSI_ERR_INVALID_ARG;
   if (kv_len == lens || n_new == kv_len || n_new == lens) return GSI_ERR_INVALID_ARG;
   const gsi_status_t st = on_device(h);
   if (st != GSI_OK) return st;
-  const kv::PlanArgs a{n_new, n_seqs, commit, lens, n_free, free_pages, table, q_start, kv_len, slots, positions, counts};
+  const kv::PlanArgs a{n_new, n_seqs, commit & GSI_KV_ALL_SEQS ? h->shape.max_seqs : n_seqs, commit & GSI_KV_COMMIT, lens, n_free, free_pages, table, q_start, kv_len, slots, positions, counts};
+  h->planned = n_seqs;
   return launched(h, stream, kv::launch_plan(h->shape, a, h->ctl, stream));
 }
 
@@ -745,7 +752,7 @@ gsi_status_t gsi_kv_attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t
   if (st != GSI_OK) return st;
   const kv::AttendArgs a{q, out, dtype, q_token_stride, q_head_stride, out_token_stride, out_head_stride, n_rows, n_q_heads,
                          n_q_heads / h->shape.n_heads, 1.f / (n_q_heads / h->shape.n_heads), aligned(q, 16) && ((q_token_stride | q_head_stride) * size_of(dtype) & 15) == 0,
-                         (float)(scale * 1.4426950408889634), q_start, kv_len, table, n_seqs, static_cast<const unsigned char*>(pages),
+                         (float)(scale * 1.4426950408889634), q_start, kv_len, table, n_seqs, h->planned && h->planned < n_seqs ? h->planned : n_seqs, static_cast<const unsigned char*>(pages),
                          h->parts, h->tickets};
   return launched(h, stream, kv::launch_attend(h->shape, a, h->ctl, stream));
 }

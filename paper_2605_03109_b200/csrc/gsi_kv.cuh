@@ -58,7 +58,7 @@ struct Control {          // at the front of the workspace
 
 struct PlanArgs {
   const int* n_new;
-  int n_seqs, commit;
+  int n_seqs, upto, commit;   // upto: the requests that q_start and kv_len are written for
   int *lens, *n_free;
   const int* free_pages;
   int *table, *q_start, *kv_len, *slots, *positions, *counts;
@@ -86,7 +86,7 @@ struct AttendArgs {
   bool q_vec;                      // eight channels of q lie on 16 bytes
   float scale;   // of scores in powers of two
   const int *q_start, *kv_len, *table;
-  int n_seqs;
+  int n_seqs, likely;   // likely: how many of them have rows, for the choice of a form
   const unsigned char* pages;
   float* parts;        // [kMaxShares][2]: what a warp has of a segment begun before its share, and of one that ends behind it
   unsigned* tickets;   // [kMaxShares]

@@ -1108,8 +1108,8 @@ cudaError_t prepare_attend(const Shape& s) {
 
 cudaError_t launch_attend(const Shape& s, const AttendArgs& a, Control* ctl, cudaStream_t stream) {
   // The smallest unit that holds the rows of a sequence on average (half a row left over may go to a second tile of rows:
-  // batches are padded).
-  const double mean = (double)a.n_rows * a.shared / a.n_seqs - 0.5;
+  // batches are padded); requests as in the last plan, though all are looked at.
+  const double mean = (double)a.n_rows * a.shared / a.likely - 0.5;
   int rows = 1;
   while (rows < 8 && rows * (a.dtype == GSI_F32 ? 1 : 2) < mean) rows *= 2;
   return launch_any(a.dtype, rows, s, a, ctl, stream);

@@ -207,7 +207,7 @@ PyObject* py_bind(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
 // ---- the cache of keys and values: a handle and the tensors of its state, in a capsule
 struct Cache {
   gsi_kv_t handle = nullptr;
-  int64_t n_heads = 0, head_dim = 0, max_seqs = 0, layers = 0, n_seqs = 0;
+  int64_t n_heads = 0, head_dim = 0, max_seqs = 0, layers = 0;
   at::Tensor pages, table, lens, free, n_free, q_start, kv_len, slots, positions, counts;
   c10::Device device = c10::Device(c10::kCPU);
 };
@@ -269,7 +269,7 @@ PyObject* py_kv_state(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     *to[i] = *t;
   }
   c->device = c->pages.device();
-  c->max_seqs = c->n_seqs = c->lens.numel();
+  c->max_seqs = c->lens.numel();
   return PyCapsule_New(c.release(), kCacheName, [](PyObject* o) { delete static_cast<Cache*>(PyCapsule_GetPointer(o, kCacheName)); });
   END_HANDLE_TH_ERRORS
 }
@@ -295,11 +295,11 @@ PyObject* py_kv_plan(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   {
     NoGil no_gil;
     const c10::cuda::CUDAGuard guard(c->device);
-    status = kv_plan(c->handle, ptr<int>(*n_new), (int)n_new->numel(), commit, ptr<int>(c->lens), ptr<int>(c->n_free), ptr<int>(c->free),
+    // (for all requests: what comes after goes by the tensors alone, whichever plan a replayed graph has run)
+    status = kv_plan(c->handle, ptr<int>(*n_new), (int)n_new->numel(), GSI_KV_ALL_SEQS | (commit ? GSI_KV_COMMIT : 0), ptr<int>(c->lens), ptr<int>(c->n_free), ptr<int>(c->free),
                      ptr<int>(c->table), ptr<int>(c->q_start), ptr<int>(c->kv_len), ptr<int>(c->slots), ptr<int>(c->positions),
                      ptr<int>(c->counts), stream_on(*c, given, stream));
   }
-  if (status == GSI_OK) c->n_seqs = n_new->numel();
   return PyLong_FromLong(status);
   END_HANDLE_TH_ERRORS
 }
@@ -398,7 +398,7 @@ PyObject* py_kv_attend(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     const c10::cuda::CUDAGuard guard(c->device);
     if (!out.defined()) out = at::empty({q->size(0), q->size(1), q->size(2)}, q->options());
     status = kv_attend(c->handle, q->data_ptr(), type, q->stride(0), q->stride(1), (int)q->size(0), (int)q->size(1), (float)scale,
-                       ptr<int>(c->q_start), ptr<int>(c->kv_len), ptr<int>(c->table), (int)c->n_seqs, pages, out.data_ptr(), out.stride(0),
+                       ptr<int>(c->q_start), ptr<int>(c->kv_len), ptr<int>(c->table), (int)c->max_seqs, pages, out.data_ptr(), out.stride(0),
                        out.stride(1), stream_on(*c, given, stream));
   }
   return Py_BuildValue("iN", status, THPVariable_Wrap(out));

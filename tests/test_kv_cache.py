@@ -943,3 +943,81 @@ def test_hundreds_of_sets_of_tiles_a_warp(dtype, dim, heads, seqs, new, length):
             want, off = R.attend_of_long_shares(qn[i * new + m, h], *[[y[:sees, 0] for y in z] for z in (k, v)], dim ** -0.5, dtype != torch.float32, sets, parts)
             tol = off + half * np.abs(want) + (3e-8 if dtype == torch.float16 else 0)
             assert (np.abs(got[i * new + m, h] - want) <= tol).all(), (i, h, m, float((np.abs(got[i * new + m, h] - want) / tol).max()))
+
+
+def planned(c, lens):
+    """Tokens in an empty cache for requests of `lens`."""
+    c.plan(ints(lens))
+    k, v = (torch.randn(sum(lens), c.n_heads, c.head_dim, device="cuda") for _ in range(2))
+    c.append(k, v)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_an_attention_goes_by_the_plan_that_ran_last(dtype):
+    """Plans of eight requests and of four, captured and not, before an attention that was captured behind the other."""
+    g, rng = gsi(), np.random.default_rng(51)
+    lens = [40, 3, 100, 17, 5, 64, 1, 30]
+    for captured, last in (([1] * 8, [3, 1, 1, 1]), ([3, 1, 1, 1], [1] * 8), ([2, 0, 1], [1] * 8)):
+        c = g.KVCache(2, 64, 64, 8, 200, page_tokens=16, max_tokens=300)
+        planned(c, lens)
+        q = rows(rng, (10, 4, 64), dtype)
+        out = torch.full_like(q, 9.0)
+        first, then = ints(captured), ints(last)
+
+        def expect():
+            """From the tensors alone."""
+            starts, kv_len, table = c.q_start.cpu().tolist(), c.kv_len.cpu().tolist(), c.table.cpu().numpy().astype(np.int64)
+            news = [b - a for a, b in zip(starts, starts[1:])]
+            return read_back(c, slots_of(c, kv_len, table)), kv_len, news
+
+        c.plan(first)
+        c.append(*(torch.randn(sum(captured), 2, 64, device="cuda") for _ in range(2)))
+        c.attend(q, out=out)
+        torch.cuda.synchronize()
+        plan_graph, attend_graph = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(plan_graph):
+            c.plan(first, commit=False)
+        with torch.cuda.graph(attend_graph):
+            c.attend(q, out=out)
+        for replay in (False, True):         # eager, and replayed attention behind an eager plan of another number
+            c.plan(then, commit=False)
+            assert c.q_start.cpu().tolist()[len(last):] == [sum(last)] * (9 - len(last)) and not c.kv_len[len(last):].any()
+            new = torch.randn(sum(last), 2, 64, device="cuda")
+            c.append(new, new)
+            out.fill_(9.0)
+            attend_graph.replay() if replay else c.attend(q, out=out)
+            check(c, q, out, torch.full_like(q, 9.0), *expect(), 0.125)
+            # ... and an eager one behind the replayed plan
+            plan_graph.replay()
+            assert c.counts.cpu().tolist()[0] == sum(captured)
+            new = torch.randn(sum(captured), 2, 64, device="cuda")
+            c.append(new, new)
+            out.fill_(9.0)
+            attend_graph.replay() if replay else c.attend(q, out=out)
+            check(c, q, out, torch.full_like(q, 9.0), *expect(), 0.125)
+        assert c.status() == 0
+
+
+@gpu
+def test_a_plan_of_the_library_writes_what_it_is_asked_for():
+    """Without GSI_KV_ALL_SEQS: nothing behind its own requests; flags that there are not are refused."""
+    from paper_2605_03109_b200 import binding
+    g = gsi()
+    c = g.KVCache(1, 64, 16, 6, 64, page_tokens=16, max_tokens=8)
+    n_new = ints([2, 1, 3])
+
+    def plan(commit):
+        return g.lib.gsi_kv_plan(c.handle, n_new.data_ptr(), 3, commit, c.lens.data_ptr(), c.n_free.data_ptr(), c.free.data_ptr(), c.table.data_ptr(),
+                                 c.q_start.data_ptr(), c.kv_len.data_ptr(), c.slots.data_ptr(), c.positions.data_ptr(), c.counts.data_ptr(),
+                                 binding._stream_ptr(None))
+
+    for commit, behind in ((0, False), (1, False), (2, True), (3, True)):
+        c.q_start.fill_(77)
+        c.kv_len.fill_(77)
+        before = c.lens.clone()
+        assert plan(commit) == 0
+        assert c.q_start.cpu().tolist() == [0, 2, 3, 6] + [6 if behind else 77] * 3
+        assert c.kv_len.cpu().tolist()[:3] == (before[:3] + n_new).cpu().tolist() and c.kv_len.cpu().tolist()[3:] == [0 if behind else 77] * 3
+        assert torch.equal(c.lens - before, torch.cat([n_new, ints([0] * 3)]) * (commit & 1))
+    assert plan(4) == plan(-1) == 1
