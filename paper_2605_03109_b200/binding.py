@@ -7,6 +7,7 @@ the import fails loudly: there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -421,15 +422,18 @@ class KVCache:
         if dev.index is None:
             dev = torch.device("cuda", torch.cuda.current_device())
         whole = self.n_layers * self.n_pages * self.page_bytes
+        # (what is made here is filled on the stream that gsi_kv_create waits for)
+        on = contextlib.nullcontext() if stream is None else torch.cuda.stream(torch.cuda.ExternalStream(_stream_ptr(stream), dev))
         if pages is None:
-            pages = torch.empty((self.n_layers, self.n_pages, self.page_bytes), dtype=torch.uint8, device=dev)
+            with on:
+                pages = torch.empty((self.n_layers, self.n_pages, self.page_bytes), dtype=torch.uint8, device=dev)
         assert pages.dtype == torch.uint8 and pages.is_contiguous() and pages.numel() == whole and pages.data_ptr() % 16 == 0
         self.device, self.pages = dev, pages
 
         def ints(*shape, fill=0):
             return torch.full(shape, fill, dtype=torch.int32, device=dev)
 
-        with torch.cuda.device(dev):
+        with torch.cuda.device(dev), on:
             self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
             self.table, self.lens = ints(int(max_seqs), max_pages, fill=-1), ints(int(max_seqs))
             self.free = torch.arange(self.n_pages - 1, -1, -1, dtype=torch.int32, device=dev)

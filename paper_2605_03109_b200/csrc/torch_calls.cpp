@@ -13,6 +13,7 @@
 #include <memory>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -82,6 +83,20 @@ bool enough(Py_ssize_t given, Py_ssize_t wanted) {
   if (given == wanted) return true;
   PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
   return false;
+}
+
+// A tensor that the kernels of a stream write (`given`: one that is not torch's current one, perhaps).  It is of that stream's
+// memory, as what is free to the current stream may still be in use there, and is not handed out again before the current stream,
+// whose tensor it is from here on, is done with it.
+at::Tensor made_on(bool given, void* stream, at::IntArrayRef size, const at::TensorOptions& options) {
+  const c10::DeviceIndex device = options.device().index();
+  const auto current = c10::cuda::getCurrentCUDAStream(device);
+  if (stream == (void*)cudaStreamLegacy) stream = nullptr;
+  if (!given || stream == (void*)current.stream()) return at::empty(size, options);
+  const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), device));
+  at::Tensor t = at::empty(size, options);
+  if (t.numel()) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), current);
+  return t;
 }
 
 void allocate(const at::Tensor& x, int64_t n, int64_t O, at::Tensor* y, at::Tensor* gate, at::Tensor* rho) {
@@ -365,8 +380,8 @@ PyObject* py_kv_read(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     NoGil no_gil;
     const c10::cuda::CUDAGuard guard(c->device);
     const auto options = slots->options().dtype(like->scalar_type());
-    k = at::empty({slots->numel(), c->n_heads, c->head_dim}, options);
-    v = at::empty({slots->numel(), c->n_heads, c->head_dim}, options);
+    k = made_on(given, stream, {slots->numel(), c->n_heads, c->head_dim}, options);
+    v = made_on(given, stream, {slots->numel(), c->n_heads, c->head_dim}, options);
     status = kv_read(c->handle, pages, ptr<int>(*slots), (int)slots->numel(), type, k.data_ptr(), v.data_ptr(), stream_on(*c, given, stream));
   }
   return Py_BuildValue("iNN", status, THPVariable_Wrap(k), THPVariable_Wrap(v));
@@ -396,7 +411,7 @@ PyObject* py_kv_attend(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   {
     NoGil no_gil;
     const c10::cuda::CUDAGuard guard(c->device);
-    if (!out.defined()) out = at::empty({q->size(0), q->size(1), q->size(2)}, q->options());
+    if (!out.defined()) out = made_on(given, stream, {q->size(0), q->size(1), q->size(2)}, q->options());
     status = kv_attend(c->handle, q->data_ptr(), type, q->stride(0), q->stride(1), (int)q->size(0), (int)q->size(1), (float)scale,
                        ptr<int>(c->q_start), ptr<int>(c->kv_len), ptr<int>(c->table), (int)c->max_seqs, pages, out.data_ptr(), out.stride(0),
                        out.stride(1), stream_on(*c, given, stream));

@@ -1021,3 +1021,59 @@ def test_a_plan_of_the_library_writes_what_it_is_asked_for():
         assert c.kv_len.cpu().tolist()[:3] == (before[:3] + n_new).cpu().tolist() and c.kv_len.cpu().tolist()[3:] == [0 if behind else 77] * 3
         assert torch.equal(c.lens - before, torch.cat([n_new, ints([0] * 3)]) * (commit & 1))
     assert plan(4) == plan(-1) == 1
+
+
+@gpu
+def test_outputs_are_of_the_memory_of_the_stream_that_writes_them():
+    """Memory that the current stream has given back may still be in use there; an output's own goes back when both streams are done with it."""
+    rng = np.random.default_rng(61)
+    kv_len, news = [900, 17], [40, 8]
+    c, table = a_cache(2, 128, 16, kv_len, news, rng)
+    kv = fill_and_read(c, rng, kv_len, table)
+    q = rows(rng, (48, 4, 128), torch.float32)
+    want = c.attend(q)
+    check(c, q, want, want, kv, kv_len, news, 128 ** -0.5)
+    slots = torch.from_numpy(slots_of(c, kv_len, table)[:48]).cuda()
+    values = c.read(slots)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for call, given in ((lambda s: [c.attend(q, stream=s)], want), (lambda s: c.read(slots, stream=s), values[0])):
+        for stream in (side, side.cuda_stream):
+            old = [torch.full_like(given, 3.0) for _ in range(8)]
+            places = {x.data_ptr() for x in old}
+            torch.cuda._sleep(20_000_000)                 # (some 10 ms)
+            sums = [x.sum() for x in old]
+            del old
+            got = call(stream)
+            assert not places & {x.data_ptr() for x in got}
+            side.synchronize()
+            assert all(torch.equal(x, y) for x, y in zip(got, [want] if len(got) == 1 else values))
+            assert all(x.item() == 3.0 * given.numel() for x in sums)
+            # used by the current stream, given back, asked for again
+            places = {x.data_ptr() for x in got}
+            torch.cuda._sleep(20_000_000)
+            sums = [x.double().sum() for x in got]
+            del got
+            again = call(stream)
+            assert not places & {x.data_ptr() for x in again}
+            torch.cuda.synchronize()
+            assert [x.item() for x in sums] == [x.double().sum().item() for x in again]
+    assert c.status() == 0
+
+
+@gpu
+def test_a_cache_made_on_another_stream_is_ready_there():
+    g, side = gsi(), torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        torch.cuda._sleep(100_000_000)                    # the current stream is busy (some 50 ms)
+        c = g.KVCache(2, 64, 8, 2, 64, page_tokens=16, max_tokens=40, stream=stream)
+        with torch.cuda.stream(side):
+            n_new = ints([33, 7])
+            q, k, v = (torch.randn(40, 2, 64, device="cuda") for _ in range(3))
+            c.plan(n_new)
+            c.append(k, v)
+            out = c.attend(q)
+        side.synchronize()
+        lens = [33, 7]
+        check(c, q, out, out, read_back(c, slots_of(c, lens, c.table.cpu().numpy().astype(np.int64))), lens, lens, 0.125)
+        assert c.counts.cpu().tolist() == [40, 4, 4, 0] and c.status() == 0
