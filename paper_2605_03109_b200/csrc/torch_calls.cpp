@@ -99,10 +99,10 @@ at::Tensor made_on(bool given, void* stream, at::IntArrayRef size, const at::Ten
   return t;
 }
 
-void allocate(const at::Tensor& x, int64_t n, int64_t O, at::Tensor* y, at::Tensor* gate, at::Tensor* rho) {
-  if (!y->defined()) *y = at::empty({n, O}, x.options());
-  if (!gate->defined()) *gate = at::empty({n}, x.options().dtype(at::kByte));
-  if (!rho->defined()) *rho = at::empty({n}, x.options());
+void allocate(bool given, void* stream, const at::Tensor& x, int64_t n, int64_t O, at::Tensor* y, at::Tensor* gate, at::Tensor* rho) {
+  if (!y->defined()) *y = made_on(given, stream, {n, O}, x.options());
+  if (!gate->defined()) *gate = made_on(given, stream, {n}, x.options().dtype(at::kByte));
+  if (!rho->defined()) *rho = made_on(given, stream, {n}, x.options());
 }
 
 // forward(handle, O, x, y, gate, rho, stream) -> (status, y, gate, rho)
@@ -123,7 +123,7 @@ PyObject* py_forward(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   {
     NoGil no_gil;
     const int64_t n = x->size(0);
-    allocate(*x, n, O, &y, &gate, &rho);
+    allocate(given, stream, *x, n, O, &y, &gate, &rho);
     if (!given) stream = c10::cuda::getCurrentCUDAStream().stream();
     status = forward_n(handle, static_cast<const float*>(x->data_ptr()), (int)n, static_cast<float*>(y.data_ptr()),
                        static_cast<unsigned char*>(gate.data_ptr()), static_cast<float*>(rho.data_ptr()),
@@ -153,8 +153,8 @@ PyObject* py_extend(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   int status;
   {
     NoGil no_gil;
-    appended = at::empty({1}, x->options().dtype(at::kInt));
-    rho = at::empty({1}, x->options());
+    appended = made_on(given, stream, {1}, x->options().dtype(at::kInt));
+    rho = made_on(given, stream, {1}, x->options());
     if (!given) stream = c10::cuda::getCurrentCUDAStream().stream();
     status = extend_basis(handle, static_cast<const float*>(x->data_ptr()), (float)tau,
                           static_cast<int*>(k_active->data_ptr()), static_cast<int*>(appended.data_ptr()),
@@ -198,7 +198,7 @@ PyObject* py_forward_static(PyObject*, PyObject* const* args, Py_ssize_t n_args)
   {
     NoGil no_gil;
     const int64_t n = x->size(0);
-    allocate(*x, n, O, &y, &gate, &rho);
+    allocate(given, stream, *x, n, O, &y, &gate, &rho);
     if (!given) stream = c10::cuda::getCurrentCUDAStream().stream();
     status = forward_static(W.data(), d_out.data(), (int)maps, P->data_ptr(), (gsi_dtype_t)p_dtype, W_P->data_ptr(),
                             (int)P->size(0), (int)P->size(1), (float)eps, static_cast<const float*>(x->data_ptr()), (int)n,

@@ -2054,3 +2054,40 @@ def test_calls_refuse_and_accept_what_their_arguments_say():
     closed.close()
     with pytest.raises(g.GsiError):
         closed.forward(xd)
+
+
+def test_outputs_of_a_call_are_of_the_memory_of_its_stream():
+    """What the current stream has given back may still be in use there; an output goes back when both streams are done with it."""
+    g = G()
+    x, P, Ws = make_small(256, 64, (2048, 1024), 2, seed=9991, outlier_every=2)
+    xd, Pd, Wd = x.cuda(), P.cuda(), [W.cuda() for W in Ws]
+    lay = g.Layer(Wd, Pd, 0.05, max_tokens=2)
+    wp = torch.cat([g.gsi_build_image(W, Pd) for W in Wd])
+    ka = torch.tensor([64], dtype=torch.int32, device="cuda")       # (no room left: nothing is appended)
+    side = torch.cuda.Stream()
+    calls = [lambda s: lay.forward(xd, stream=s), lambda s: g.gsi_forward_static(Wd, Pd, wp, 0.05, xd, stream=s),
+             lambda s: lay.extend_basis(xd[0], 0.5, ka, stream=s)]
+    for call in calls:
+        want = [t.clone() for t in call(None)]
+        torch.cuda.synchronize()
+        for stream in (side, side.cuda_stream):
+            old = [torch.full_like(t, 3) for t in want for _ in range(8)]
+            places = {t.data_ptr() for t in old}
+            torch.cuda._sleep(20_000_000)                           # (some 10 ms)
+            sums = [t.double().sum() for t in old]
+            sizes = [t.numel() for t in old]
+            del old
+            got = call(stream)
+            assert not places & {t.data_ptr() for t in got}
+            side.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            assert [s.item() for s in sums] == [3.0 * n for n in sizes]
+            places = {t.data_ptr() for t in got}
+            torch.cuda._sleep(20_000_000)
+            sums = [t.double().sum() for t in got]
+            del got
+            again = call(stream)
+            assert not places & {t.data_ptr() for t in again}
+            torch.cuda.synchronize()
+            assert [s.item() for s in sums] == [t.double().sum().item() for t in again]
+    assert lay.status() == 0 and ka.item() == 64
