@@ -563,6 +563,12 @@ gsi_status_t gsi_kv_attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t
                            const int* kv_len, const int* table, int n_seqs, const void* pages, void* out,
                            int64_t out_token_stride, int64_t out_head_stride, gsi_stream_t stream);
 
+/* The same, and the rows behind the last sequence's, q_start[n_seqs] .. n_rows - 1, become zeros. */
+gsi_status_t gsi_kv_attend_all(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t q_token_stride,
+                               int64_t q_head_stride, int n_rows, int n_q_heads, float scale, const int* q_start,
+                               const int* kv_len, const int* table, int n_seqs, const void* pages, void* out,
+                               int64_t out_token_stride, int64_t out_head_stride, gsi_stream_t stream);
+
 /* Synchronises the handle's last stream and returns the status word, which stays set.  After GSI_ERR_TIMEOUT (a copy within
  * the GPU did not arrive for seconds) the outputs of that call are undefined and the handle has to be made again. */
 gsi_status_t gsi_kv_get_status(gsi_kv_t h, int* device_status);

@@ -27,7 +27,7 @@ EXPORTED = [
     "gsi_stack_set_mode", "gsi_stack_set_concurrent", "gsi_stack_is_persistent", "gsi_stack_set_trace", "gsi_stack_set_spin_limit", "gsi_stack_seek", "gsi_stack_step", "gsi_stack_launches_per_step",
     "gsi_stack_step_host", "gsi_stack_get_status", "gsi_stack_destroy",
     "gsi_kv_page_bytes", "gsi_kv_workspace_bytes", "gsi_kv_locate", "gsi_kv_create", "gsi_kv_plan", "gsi_kv_release",
-    "gsi_kv_append", "gsi_kv_read", "gsi_kv_attend", "gsi_kv_get_status", "gsi_kv_destroy",
+    "gsi_kv_append", "gsi_kv_read", "gsi_kv_attend", "gsi_kv_attend_all", "gsi_kv_get_status", "gsi_kv_destroy",
 ]
 
 
@@ -100,7 +100,7 @@ def _load():
     l.gsi_kv_release.argtypes = [vp, vp, i, vp, vp, vp, vp, vp]
     l.gsi_kv_append.argtypes = [vp, vp, vp, i, ll, ll, ll, ll, vp, i, vp, vp]
     l.gsi_kv_read.argtypes = [vp, vp, vp, i, i, vp, vp, vp]
-    l.gsi_kv_attend.argtypes = [vp, vp, i, ll, ll, i, i, C.c_float, vp, vp, vp, i, vp, vp, ll, ll, vp]
+    l.gsi_kv_attend.argtypes = l.gsi_kv_attend_all.argtypes = [vp, vp, i, ll, ll, i, i, C.c_float, vp, vp, vp, i, vp, vp, ll, ll, vp]
     l.gsi_kv_get_status.argtypes = [vp, C.POINTER(i)]
     l.gsi_kv_destroy.argtypes = [vp]
     for name in EXPORTED:
@@ -117,7 +117,7 @@ def _load_calls():
     spec.loader.exec_module(m)
     m.bind(*[C.cast(f, C.c_void_p).value for f in (lib.gsi_forward_n, lib.gsi_extend_basis, lib.gsi_forward_static)])
     m.bind_kv(*[C.cast(f, C.c_void_p).value for f in (lib.gsi_kv_plan, lib.gsi_kv_release, lib.gsi_kv_append, lib.gsi_kv_read,
-                                                      lib.gsi_kv_attend)])
+                                                      lib.gsi_kv_attend, lib.gsi_kv_attend_all)])
     return m
 
 
@@ -470,7 +470,8 @@ class KVCache:
 
     def attend(self, q: torch.Tensor, layer: int = 0, scale: float | None = None, out: torch.Tensor | None = None, stream=None):
         """Attention of the plan's rows, each over its request's tokens up to its own; ``scale`` is
-        ``head_dim ** -0.5`` by default.  Rows behind the last request's are not written.  ``out`` shares no element with ``q``."""
+        ``head_dim ** -0.5`` by default.  ``out`` shares no element with ``q``; its rows behind the last request's are
+        not written (without ``out``: zeros)."""
         status, out = _calls.kv_attend(self._state, q, layer, self._scale if scale is None else scale, out, stream)
         if status:
             _check(status, "gsi_kv_attend")

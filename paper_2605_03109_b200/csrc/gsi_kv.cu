@@ -629,6 +629,26 @@ gsi_status_t launched(gsi_kv_t h, cudaStream_t stream, cudaError_t e) {
   h->last_stream = stream;
   return e == cudaSuccess ? GSI_OK : GSI_ERR_CUDA;
 }
+gsi_status_t attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t q_token_stride, int64_t q_head_stride, int n_rows, int n_q_heads, float scale,
+                    const int* q_start, const int* kv_len, const int* table, int n_seqs, const void* pages, void* out, int64_t out_token_stride,
+                    int64_t out_head_stride, bool clear, gsi_stream_t stream) {
+  if (!h || !is_type(dtype) || n_rows < 0 || n_q_heads <= 0 || n_q_heads % h->shape.n_heads || n_seqs <= 0 || n_seqs > h->shape.max_seqs ||
+      !std::isfinite(scale))
+    return GSI_ERR_INVALID_ARG;
+  if ((long long)n_rows * n_q_heads >= 1ll << 31 || n_q_heads / h->shape.n_heads > kv::kMaxShared) return GSI_ERR_UNSUPPORTED;
+  if (n_rows == 0) return GSI_OK;
+  if (!aligned(q, size_of(dtype)) || !aligned(out, size_of(dtype)) || !aligned(pages, 16)) return GSI_ERR_INVALID_ARG;
+  for (const int* p : {q_start, kv_len, table})
+    if (!aligned(p, 4)) return GSI_ERR_INVALID_ARG;
+  if (q_token_stride < 0 || q_head_stride < 0 || out_token_stride < 0 || out_head_stride < 0) return GSI_ERR_INVALID_ARG;
+  const gsi_status_t st = on_device(h);
+  if (st != GSI_OK) return st;
+  const kv::AttendArgs a{q, out, dtype, q_token_stride, q_head_stride, out_token_stride, out_head_stride, n_rows, n_q_heads,
+                         n_q_heads / h->shape.n_heads, 1.f / (n_q_heads / h->shape.n_heads), aligned(q, 16) && ((q_token_stride | q_head_stride) * size_of(dtype) & 15) == 0,
+                         (float)(scale * 1.4426950408889634), q_start, kv_len, table, n_seqs, h->planned && h->planned < n_seqs ? h->planned : n_seqs, static_cast<const unsigned char*>(pages),
+                         clear, h->parts, h->tickets};
+  return launched(h, stream, kv::launch_attend(h->shape, a, h->ctl, stream));
+}
 
 }  // namespace
 
@@ -739,22 +759,15 @@ gsi_status_t gsi_kv_read(gsi_kv_t h, const void* pages, const int* slots, int n,
 gsi_status_t gsi_kv_attend(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t q_token_stride, int64_t q_head_stride, int n_rows,
                            int n_q_heads, float scale, const int* q_start, const int* kv_len, const int* table, int n_seqs,
                            const void* pages, void* out, int64_t out_token_stride, int64_t out_head_stride, gsi_stream_t stream) {
-  if (!h || !is_type(dtype) || n_rows < 0 || n_q_heads <= 0 || n_q_heads % h->shape.n_heads || n_seqs <= 0 || n_seqs > h->shape.max_seqs ||
-      !std::isfinite(scale))
-    return GSI_ERR_INVALID_ARG;
-  if ((long long)n_rows * n_q_heads >= 1ll << 31 || n_q_heads / h->shape.n_heads > kv::kMaxShared) return GSI_ERR_UNSUPPORTED;
-  if (n_rows == 0) return GSI_OK;
-  if (!aligned(q, size_of(dtype)) || !aligned(out, size_of(dtype)) || !aligned(pages, 16)) return GSI_ERR_INVALID_ARG;
-  for (const int* p : {q_start, kv_len, table})
-    if (!aligned(p, 4)) return GSI_ERR_INVALID_ARG;
-  if (q_token_stride < 0 || q_head_stride < 0 || out_token_stride < 0 || out_head_stride < 0) return GSI_ERR_INVALID_ARG;
-  const gsi_status_t st = on_device(h);
-  if (st != GSI_OK) return st;
-  const kv::AttendArgs a{q, out, dtype, q_token_stride, q_head_stride, out_token_stride, out_head_stride, n_rows, n_q_heads,
-                         n_q_heads / h->shape.n_heads, 1.f / (n_q_heads / h->shape.n_heads), aligned(q, 16) && ((q_token_stride | q_head_stride) * size_of(dtype) & 15) == 0,
-                         (float)(scale * 1.4426950408889634), q_start, kv_len, table, n_seqs, h->planned && h->planned < n_seqs ? h->planned : n_seqs, static_cast<const unsigned char*>(pages),
-                         h->parts, h->tickets};
-  return launched(h, stream, kv::launch_attend(h->shape, a, h->ctl, stream));
+  return attend(h, q, dtype, q_token_stride, q_head_stride, n_rows, n_q_heads, scale, q_start, kv_len, table, n_seqs, pages, out, out_token_stride,
+                out_head_stride, false, stream);
+}
+
+gsi_status_t gsi_kv_attend_all(gsi_kv_t h, const void* q, gsi_dtype_t dtype, int64_t q_token_stride, int64_t q_head_stride, int n_rows,
+                               int n_q_heads, float scale, const int* q_start, const int* kv_len, const int* table, int n_seqs,
+                               const void* pages, void* out, int64_t out_token_stride, int64_t out_head_stride, gsi_stream_t stream) {
+  return attend(h, q, dtype, q_token_stride, q_head_stride, n_rows, n_q_heads, scale, q_start, kv_len, table, n_seqs, pages, out, out_token_stride,
+                out_head_stride, true, stream);
 }
 
 gsi_status_t gsi_kv_get_status(gsi_kv_t h, int* device_status) {

@@ -88,6 +88,7 @@ struct AttendArgs {
   const int *q_start, *kv_len, *table;
   int n_seqs, likely;   // likely: how many of them have rows, for the choice of a form
   const unsigned char* pages;
+  bool clear;          // rows behind the last request's become zeros
   float* parts;        // [kMaxShares][2]: what a warp has of a segment begun before its share, and of one that ends behind it
   unsigned* tickets;   // [kMaxShares]
 };

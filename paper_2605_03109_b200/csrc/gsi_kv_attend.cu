@@ -232,6 +232,13 @@ __global__ void __launch_bounds__(Cfg<G, kColumns<kType>, L, NT>::kThreads, 1) k
   pdl_launch_dependents();
   pdl_wait();
 
+  if (a.clear) {
+    const long long width = (long long)a.n_q_heads * s.head_dim;
+    for (long long row = max(a.q_start[a.n_seqs], 0) + (long long)blockIdx.x; row < a.n_rows; row += gridDim.x)
+      for (long long i = tid; i < width; i += kThreads)
+        store_from_float(a.out, kType, row * a.out_token + i / s.head_dim * a.out_head + i % s.head_dim, 0.f);
+  }
+
   // ---- shares: the units of all sequences in order, in even pieces that end with a segment where one ends near.  A segment
   // counts as kCost units more: its rows have to be fetched and its sums to be put away.
   Scan2 total;

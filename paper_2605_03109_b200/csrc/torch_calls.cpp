@@ -31,6 +31,7 @@ decltype(&gsi_kv_release) kv_release = nullptr;
 decltype(&gsi_kv_append) kv_append = nullptr;
 decltype(&gsi_kv_read) kv_read = nullptr;
 decltype(&gsi_kv_attend) kv_attend = nullptr;
+decltype(&gsi_kv_attend_all) kv_attend_all = nullptr;
 
 struct NoGil {
   PyThreadState* state = PyEval_SaveThread();
@@ -411,22 +412,24 @@ PyObject* py_kv_attend(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   {
     NoGil no_gil;
     const c10::cuda::CUDAGuard guard(c->device);
-    if (!out.defined()) out = made_on(given, stream, {q->size(0), q->size(1), q->size(2)}, q->options());
-    status = kv_attend(c->handle, q->data_ptr(), type, q->stride(0), q->stride(1), (int)q->size(0), (int)q->size(1), (float)scale,
+    const bool made = !out.defined();   // (whose rows behind the last request's are written, too)
+    if (made) out = made_on(given, stream, {q->size(0), q->size(1), q->size(2)}, q->options());
+    status = (made ? kv_attend_all : kv_attend)(c->handle, q->data_ptr(), type, q->stride(0), q->stride(1), (int)q->size(0), (int)q->size(1), (float)scale,
                        ptr<int>(c->q_start), ptr<int>(c->kv_len), ptr<int>(c->table), (int)c->max_seqs, pages, out.data_ptr(), out.stride(0),
                        out.stride(1), stream_on(*c, given, stream));
   }
   return Py_BuildValue("iN", status, THPVariable_Wrap(out));
   END_HANDLE_TH_ERRORS
 }
-// bind_kv(addresses of gsi_kv_plan, _release, _append, _read, _attend)
+// bind_kv(addresses of gsi_kv_plan, _release, _append, _read, _attend, _attend_all)
 PyObject* py_bind_kv(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
-  if (!enough(n_args, 5)) return nullptr;
+  if (!enough(n_args, 6)) return nullptr;
   kv_plan = reinterpret_cast<decltype(kv_plan)>(PyLong_AsVoidPtr(args[0]));
   kv_release = reinterpret_cast<decltype(kv_release)>(PyLong_AsVoidPtr(args[1]));
   kv_append = reinterpret_cast<decltype(kv_append)>(PyLong_AsVoidPtr(args[2]));
   kv_read = reinterpret_cast<decltype(kv_read)>(PyLong_AsVoidPtr(args[3]));
   kv_attend = reinterpret_cast<decltype(kv_attend)>(PyLong_AsVoidPtr(args[4]));
+  kv_attend_all = reinterpret_cast<decltype(kv_attend_all)>(PyLong_AsVoidPtr(args[5]));
   if (PyErr_Occurred()) return nullptr;
   Py_RETURN_NONE;
 }

@@ -1077,3 +1077,31 @@ def test_a_cache_made_on_another_stream_is_ready_there():
         lens = [33, 7]
         check(c, q, out, out, read_back(c, slots_of(c, lens, c.table.cpu().numpy().astype(np.int64))), lens, lens, 0.125)
         assert c.counts.cpu().tolist() == [40, 4, 4, 0] and c.status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_without_a_request_are_zeros_in_a_new_tensor(dtype):
+    """Padded batches, requests that pause: no memory that was never written reaches the next map."""
+    rng = np.random.default_rng(71)
+    kv_len, news = [30, 0, 7], [2, 0, 1]
+    c, table = a_cache(2, 64, 16, kv_len, news, rng)
+    kv = fill_and_read(c, rng, kv_len, table)
+    q = rows(rng, (8, 4, 64), dtype)
+    side = torch.cuda.Stream()
+    for stream in (None, side):
+        with torch.cuda.stream(stream):
+            for _ in range(3):
+                old = [torch.full_like(q, float("nan")) for _ in range(4)]
+                del old
+                out = c.attend(q, stream=stream)
+        torch.cuda.synchronize()
+        check(c, q, out, torch.zeros_like(out), kv, kv_len, news, 0.125)
+        assert not out[3:].any()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = c.attend(q)
+    for _ in range(2):
+        out.fill_(float("nan"))
+        graph.replay()
+        check(c, q, out, torch.zeros_like(out), kv, kv_len, news, 0.125)
