@@ -446,9 +446,12 @@ gsi_status_t gsi_stack_destroy(gsi_stack_t s);
  *   code = clamp(rint((x - mid) / s) + 8, 0, 15), 8 where s = 0
  *   value = s (code - 8) + mid
  * every step a single fp32 operation, conversions to nearest even.  Where one of
- * the 64 is not finite, s = mid = NaN, and all of them read as NaN.  So an element
- * is off by s / 2 and the rounding of mid, 2^-11 |mid| at most (and by 2^-11 of
- * 8 s from the rounding of s, where codes clamp).
+ * the 64 is not finite, s = mid = NaN, and all of them read as NaN.  While neither
+ * s nor mid saturates, an element is off by
+ *   max(s / 2, 15 ds) + dm at most,   ds = max(2^-11 s, 2^-25), dm = max(2^-11 |mid|, 2^-25)
+ * and the fp32 roundings, 2^-22 of the largest of the 64: half a step, or where codes
+ * clamp the rounding of s (2^-25 where s is subnormal in f16, or 0), and that of mid.
+ * A range above 15 x 65504, or a min + 8 s beyond +-65504, has no bound.
  *
  * Pages.  A pool is n_pages pages of gsi_kv_page_bytes(); each holds page_tokens
  * tokens of all heads: [head][tile of 16 tokens][K, V][64 channels] blocks of

@@ -149,6 +149,30 @@ def test_the_restated_numbers():
     assert (flat[0] == 8).all() and R.values(*flat)[0, 0] == np.float32(np.float16(0.3))
 
 
+def test_how_far_a_value_may_be_off():
+    """The bound that the header states: ranges from f16's subnormal steps, and below, to the largest that do not saturate,
+    centres from 0 to far outside the range; and where it ends."""
+    rng = np.random.default_rng(81)
+    n, D = 20000, 64
+    size = np.exp(rng.uniform(np.log(1e-10), np.log(3e6), (n, 1)))
+    centre = rng.choice([0.0, 1.0, -1.0], (n, 1)) * np.exp(rng.uniform(np.log(1e-9), np.log(7e4), (n, 1)))
+    shape = rng.choice(4, (n, 1))
+    x = np.where(shape == 0, rng.standard_normal((n, D)) / 4, np.where(shape == 1, rng.uniform(-1, 1, (n, D)),
+                 np.where(shape == 2, rng.choice([-1.0, 1.0], (n, D)), np.linspace(-1, 1, D))))
+    x = (x * size + centre).astype(np.float32)
+    codes, s, mid = R.quantise(x)
+    got, s, mid = R.values(codes, s, mid).astype(np.float64), s.astype(np.float64), mid.astype(np.float64)
+    off = np.abs(got - x.astype(np.float64)).max(1, keepdims=True)
+    ds, dm = np.maximum(2.0 ** -11 * s, 2.0 ** -25), np.maximum(2.0 ** -11 * np.abs(mid), 2.0 ** -25)
+    bound = np.maximum(s / 2, 15 * ds) + dm + 2.0 ** -22 * np.abs(x).max(1, keepdims=True)
+    free = (s < 65504) & (np.abs(mid) < 65504)
+    assert (off <= bound)[free].all()
+    assert (free & (s == 0)).sum() > 500 and (free & (s > 0) & (s < 2.0 ** -14)).sum() > 500 and (~free).sum() > 100
+    assert (off > s / 2 + 2.0 ** -11 * np.abs(mid) + 2.0 ** -11 * 8 * s)[free].any()      # (half a step and the normal roundings are not all)
+    assert ((x.max(1) - x.min(1) > 15 * 65472) | (np.abs(x.min(1) + 8 * s[:, 0]) > 65472))[~free[:, 0]].all()
+    assert (off > bound)[~free].any()
+
+
 # ---- on the GPU ----------------------------------------------------------------------------------------------------
 
 gpu = pytest.mark.gpu
