@@ -1129,3 +1129,58 @@ def test_rows_without_a_request_are_zeros_in_a_new_tensor(dtype):
         out.fill_(float("nan"))
         graph.replay()
         check(c, q, out, torch.zeros_like(out), kv, kv_len, news, 0.125)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,shared,dim,page,kv_len,news", [
+    (2, 1, 64, 64, [300], [300]),                                # a whole prompt
+    (1, 4, 128, 16, [257, 130, 33], [257, 1, 33]),               # prompts beside a request that goes on
+    (2, 2, 80, 48, [700, 256, 20], [256, 255, 20]),              # chunks, odd ones
+    (1, 1, 256, 64, [1000, 64], [128, 64]),
+    (1, 3, 192, 32, [129, 400], [129, 61]),
+])
+def test_chunks_and_whole_prompts(dtype, heads, shared, dim, page, kv_len, news):
+    """Many new rows of a request: each against the tokens up to its own, through plan and append as well."""
+    rng = np.random.default_rng(dim + len(kv_len))
+    g, seqs = gsi(), len(kv_len)
+    c = g.KVCache(heads, dim, sum(-(-n // page) for n in kv_len) + 3, seqs, max(kv_len), page_tokens=page, max_tokens=sum(kv_len))
+    c.pages.fill_(0xFF)
+    make = lambda n: (rows(rng, (n, heads, dim), torch.float32, 1.5), rows(rng, (n, heads, dim), torch.float32) + 0.1)  # noqa: E731
+    old = [n - m for n, m in zip(kv_len, news)]
+    if any(old):
+        c.plan(ints(old))
+        c.append(*make(sum(old)))
+    c.plan(ints(news))
+    c.append(*make(sum(news)))
+    q = rows(rng, (sum(news) + 1, heads * shared, dim), dtype, 1.3)
+    out = torch.full_like(q, 9.0)
+    c.attend(q, out=out)
+    assert (out[-1] == 9).all() and c.status() == 0 and c.kv_len.cpu().tolist() == kv_len
+    kv = read_back(c, slots_of(c, kv_len, c.table.cpu().numpy().astype(np.int64)))
+    qn, got, half = q.float().cpu().numpy(), out.double().cpu().numpy(), torch.finfo(dtype).eps / 2
+    first, row = np.concatenate([[0], np.cumsum(kv_len)]), np.concatenate([[0], np.cumsum(news)])
+    for i in range(seqs):
+        some = set(range(0, news[i], 13)) | {1, 7, 8, 15, 16, 17, 31, 32, 63, 64, news[i] - 2, news[i] - 1}
+        for m in sorted(x for x in some if 0 <= x < news[i]):
+            sees = old[i] + m + 1
+            for h in sorted({m % (heads * shared), heads * shared - 1}):
+                have = [[x[first[i]:first[i] + sees, h // shared] for x in t] for t in kv]
+                want, off = R.attend(qn[row[i] + m, h], *have, dim ** -0.5, dtype != torch.float32)
+                tol = off + half * np.abs(want) + (3e-8 if dtype == torch.float16 else 0)
+                assert (np.abs(got[row[i] + m, h] - want) <= tol).all(), (i, m, h, float((np.abs(got[row[i] + m, h] - want) / tol).max()))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_bad_page_of_a_prompt_is_that_of_the_rows_that_see_it(dtype):
+    rng = np.random.default_rng(91)
+    c, table = a_cache(2, 64, 16, [100, 40], [100, 1], rng)
+    fill(c, rng, [100, 40], table)
+    q = rows(rng, (101, 2, 64), dtype)
+    clean = c.attend(q)
+    assert c.status() == 0 and clean.isfinite().all()
+    c.table[0, 3] = -1                      # tokens 48 .. 63
+    out = c.attend(q)
+    assert torch.equal(out[:48], clean[:48]) and out[48:100].isnan().all() and torch.equal(out[100], clean[100])
+    assert c.status() == 1
