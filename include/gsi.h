@@ -455,8 +455,8 @@ gsi_status_t gsi_stack_destroy(gsi_stack_t s);
  *
  * Pages.  A pool is n_pages pages of gsi_kv_page_bytes(); each holds page_tokens
  * tokens of all heads: [head][tile of 16 tokens][K, V][64 channels] blocks of
- * 576 bytes, 512 of codes in the order of the tensor cores' operand, then the 16
- * pairs (s, mid); gsi_kv_locate gives the place of every element.  A slot is
+ * 576 bytes (a head's last one too, whatever its width), 512 of codes in the order of
+ * the tensor cores' operand, then the 16 pairs (s, mid); gsi_kv_locate gives the place of every element.  A slot is
  * page * page_tokens + token within the page.  One handle serves the pools of
  * all layers: every layer's pool has the same pages in use.
  *

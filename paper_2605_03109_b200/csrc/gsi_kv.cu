@@ -47,7 +47,7 @@ __device__ __forceinline__ bool read_last(Control* ctl, int* s_last) {
 // another; the sequences' first rows and first pages stay in shared memory, where each run of tokens and each page of the
 // block looks up its own.  The block that is last to have read the state moves it on.
 // Bound by the launch and three dependent reads (one token or 64: 3.0-3.4 us a call); prompts of 512 requests, 2.05 million tokens,
-// take 13 us, 3 of them the slots' and positions' bytes.
+// take 13 us, 3 of them the slots' and positions' bytes: after the scan 1.7 trips a thread, each a search, a page's lookup and a store in turn.
 template <int kRun>
 __global__ void __launch_bounds__(kPlanThreads) k_kv_plan(Shape s, PlanArgs a, Control* ctl) {
   extern __shared__ int sm[];
@@ -410,46 +410,46 @@ __global__ void __launch_bounds__(kRowWarps * 32, kType == GSI_F32 ? 7 : 8) k_kv
     unsigned char* first = slot >= 0 ? block_of(s, a.pages, slot, it, &t) : nullptr;
     const long long k_at = from * a.k_token + head * a.k_head, v_at = from * a.v_token + head * a.v_head;
     for (; it.group < g1; ++it.group) {
-    Quarters<kType> rows[2];
-    if (v0 == 0) rows[0].template load<kVec>(a.k, k_at + it.group * kGroup, quarter, s.head_dim - it.group * kGroup);
-    if (v1 == 2) rows[1].template load<kVec>(a.v, v_at + it.group * kGroup, quarter, s.head_dim - it.group * kGroup);
-    unsigned char* block = first + (it.group - g0) * kBlockBytes;
+      Quarters<kType> rows[2];
+      if (v0 == 0) rows[0].template load<kVec>(a.k, k_at + it.group * kGroup, quarter, s.head_dim - it.group * kGroup);
+      if (v1 == 2) rows[1].template load<kVec>(a.v, v_at + it.group * kGroup, quarter, s.head_dim - it.group * kGroup);
+      unsigned char* block = first + (it.group - g0) * kBlockBytes;
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      if (v < v0 || v >= v1) continue;
-      float lo, hi;
-      rows[v].bounds(&lo, &hi);
+      for (int v = 0; v < 2; ++v) {
+        if (v < v0 || v >= v1) continue;
+        float lo, hi;
+        rows[v].bounds(&lo, &hi);
 #pragma unroll
-      for (int o = 1; o < 4; o <<= 1) {
-        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-      }
-      const Scale z = scale_of(lo, hi);
-      uint32_t codes[4];
-      codes_of(rows[v], z, codes);
-      const uint2 code = transpose4(codes[0], codes[1], codes[2], codes[3], quarter);
-      unsigned char* to = block + v * s.groups * kBlockBytes;
-      if (first && quarter == 0) *reinterpret_cast<__half2*>(to + pair_byte(t)) = z.pair;
-      if (!v) {
-        if (first) *reinterpret_cast<uint2*>(to + k_byte(t, quarter * 16)) = code;
-        continue;
-      }
-      // V: a word is four channels of a pair of tokens; where the neighbouring lanes hold the other token of the pair,
-      // each writes one of their two octets of channels whole
-      const uint2 far = make_uint2(__shfl_xor_sync(0xffffffffu, code.x, 4), __shfl_xor_sync(0xffffffffu, code.y, 4));
-      if (!first) continue;
-      if (other >= 0 && other == (slot ^ 1)) {
-        const int odd = t & 1;
-        const uint32_t mine = odd ? code.y : code.x, theirs = odd ? far.y : far.x;
-        const uint32_t even_token = odd ? theirs : mine, odd_token = odd ? mine : theirs;
-        *reinterpret_cast<uint2*>(to + v_byte(t & ~1, quarter * 16 + odd * 8)) =
-            make_uint2(__byte_perm(even_token, odd_token, 0x5410), __byte_perm(even_token, odd_token, 0x7632));
-      } else {
+        for (int o = 1; o < 4; o <<= 1) {
+          lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+          hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        }
+        const Scale z = scale_of(lo, hi);
+        uint32_t codes[4];
+        codes_of(rows[v], z, codes);
+        const uint2 code = transpose4(codes[0], codes[1], codes[2], codes[3], quarter);
+        unsigned char* to = block + v * s.groups * kBlockBytes;
+        if (first && quarter == 0) *reinterpret_cast<__half2*>(to + pair_byte(t)) = z.pair;
+        if (!v) {
+          if (first) *reinterpret_cast<uint2*>(to + k_byte(t, quarter * 16)) = code;
+          continue;
+        }
+        // V: a word is four channels of a pair of tokens; where the neighbouring lanes hold the other token of the pair,
+        // each writes one of their two octets of channels whole
+        const uint2 far = make_uint2(__shfl_xor_sync(0xffffffffu, code.x, 4), __shfl_xor_sync(0xffffffffu, code.y, 4));
+        if (!first) continue;
+        if (other >= 0 && other == (slot ^ 1)) {
+          const int odd = t & 1;
+          const uint32_t mine = odd ? code.y : code.x, theirs = odd ? far.y : far.x;
+          const uint32_t even_token = odd ? theirs : mine, odd_token = odd ? mine : theirs;
+          *reinterpret_cast<uint2*>(to + v_byte(t & ~1, quarter * 16 + odd * 8)) =
+              make_uint2(__byte_perm(even_token, odd_token, 0x5410), __byte_perm(even_token, odd_token, 0x7632));
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<uint16_t*>(to + v_byte(t, quarter * 16 + i * 4)) = (uint16_t)((i < 2 ? code.x : code.y) >> 16 * (i & 1));
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint16_t*>(to + v_byte(t, quarter * 16 + i * 4)) = (uint16_t)((i < 2 ? code.x : code.y) >> 16 * (i & 1));
+        }
       }
-    }
     }
   }
 }

@@ -23,7 +23,7 @@
 //
 // Measured: one row of fp32, heads of 128, 240 warp instructions a tile (K and V of 16 tokens), issue slots 60 % and DRAM 94 % busy
 // once all warps run: 1.21 GB in 200 us, 6.0 TB/s.  A call has 6 us before its first tiles (lengths, shares, table, q) and
-// some 5 us of uneven ends; 604 MB of 64 ragged requests take 109 us, 125 in a loop at the card's power limit.
+// some 5 us of uneven ends; 604 MB of 64 ragged requests take 117 us, 119-127 in a loop at the card's power limit.
 #include <type_traits>
 
 #include "gsi_kv.cuh"
@@ -604,46 +604,46 @@ __global__ void __launch_bounds__(Cfg<G, kColumns<kType>, L, NT>::kThreads, 1) k
           wrong[u] = kMasked && (missing >> (u * kSet + my_tile) & 1u);
 #pragma unroll
           for (int g = 0; g < G; ++g) {
-          const uint2 pw = lds64(k_at + my_pair + (u * kSet * C::kStride + g * kBlockBytes));
-          float acc[NT][4];
+            const uint2 pw = lds64(k_at + my_pair + (u * kSet * C::kStride + g * kBlockBytes));
+            float acc[NT][4];
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            // -8 times the sum of the column's q: the sums are those of code - 8
-            if constexpr (T == 2) {
-              const float2 v = lds_float2(start_at + (g * C::kRows + row_of(n, 0)) * 8);
-              acc[n][0] = acc[n][2] = v.x;
-              acc[n][1] = acc[n][3] = v.y;
-            } else {
-              acc[n][0] = acc[n][2] = lds_float(start_at + (g * C::kRows + row_of(n, 0)) * 8);
-              acc[n][1] = acc[n][3] = lds_float(start_at + (g * C::kRows + row_of(n, 1)) * 8);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < kSet; ++i) {
-            const uint4 w = lds128(k_at + my_codes + ((u * kSet + i) * C::kStride + g * kBlockBytes));
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t x = h ? w.y : w.x, y = h ? w.w : w.z;
-              const uint32_t x8 = x >> 8, y8 = y >> 8;
-#pragma unroll
-              for (int n = 0; n < NT; ++n) {
-                const uint4 bq = lds128(q_at[i] + ((n * G + g) * 2 + h) * 512);
-                mma_f16(acc[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, bq.x, bq.y);
-                mma_f16(acc[n], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, bq.z, bq.w);
+            for (int n = 0; n < NT; ++n) {
+              // -8 times the sum of the column's q: the sums are those of code - 8
+              if constexpr (T == 2) {
+                const float2 v = lds_float2(start_at + (g * C::kRows + row_of(n, 0)) * 8);
+                acc[n][0] = acc[n][2] = v.x;
+                acc[n][1] = acc[n][3] = v.y;
+              } else {
+                acc[n][0] = acc[n][2] = lds_float(start_at + (g * C::kRows + row_of(n, 0)) * 8);
+                acc[n][1] = acc[n][3] = lds_float(start_at + (g * C::kRows + row_of(n, 1)) * 8);
               }
             }
-          }
-          const float2 p0 = unpack_half2(pw.x), p1 = unpack_half2(pw.y);   // (s, mid) of tokens gr and gr + 8
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+            for (int i = 0; i < kSet; ++i) {
+              const uint4 w = lds128(k_at + my_codes + ((u * kSet + i) * C::kStride + g * kBlockBytes));
 #pragma unroll
-            for (int r = 0; r < kLR; ++r) {
-              const float qs = lds_float(sum_at + (g * C::kRows + row_of(n, r)) * 4);
-              const float a0 = T == 2 ? fmaf(acc[n][1], 1.f / kLow, acc[n][0]) : acc[n][r];
-              const float a1 = T == 2 ? fmaf(acc[n][3], 1.f / kLow, acc[n][2]) : acc[n][2 + r];
-              S[u][n][r][0] = fmaf(p0.x, a0, g ? fmaf(p0.y, qs, S[u][n][r][0]) : p0.y * qs);
-              S[u][n][r][1] = fmaf(p1.x, a1, g ? fmaf(p1.y, qs, S[u][n][r][1]) : p1.y * qs);
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t x = h ? w.y : w.x, y = h ? w.w : w.z;
+                const uint32_t x8 = x >> 8, y8 = y >> 8;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                  const uint4 bq = lds128(q_at[i] + ((n * G + g) * 2 + h) * 512);
+                  mma_f16(acc[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, bq.x, bq.y);
+                  mma_f16(acc[n], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, bq.z, bq.w);
+                }
+              }
             }
+            const float2 p0 = unpack_half2(pw.x), p1 = unpack_half2(pw.y);   // (s, mid) of tokens gr and gr + 8
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int r = 0; r < kLR; ++r) {
+                const float qs = lds_float(sum_at + (g * C::kRows + row_of(n, r)) * 4);
+                const float a0 = T == 2 ? fmaf(acc[n][1], 1.f / kLow, acc[n][0]) : acc[n][r];
+                const float a1 = T == 2 ? fmaf(acc[n][3], 1.f / kLow, acc[n][2]) : acc[n][2 + r];
+                S[u][n][r][0] = fmaf(p0.x, a0, g ? fmaf(p0.y, qs, S[u][n][r][0]) : p0.y * qs);
+                S[u][n][r][1] = fmaf(p1.x, a1, g ? fmaf(p1.y, qs, S[u][n][r][1]) : p1.y * qs);
+              }
           }
         }
         if constexpr (C::kSplit) {
@@ -735,69 +735,69 @@ __global__ void __launch_bounds__(Cfg<G, kColumns<kType>, L, NT>::kThreads, 1) k
 #pragma unroll
         for (int u = 0; u < kSets; ++u) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int r = 0; r < kLR; ++r)
+            for (int r = 0; r < kLR; ++r)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) l[n][r] += p[u][n][r][e];
+              for (int e = 0; e < 2; ++e) l[n][r] += p[u][n][r][e];
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          const float mid0 = unpack_half2(pv[u][g].x).y, mid1 = unpack_half2(pv[u][g].y).y;
-          uint32_t b0[NT][kTerms], b1[NT][kTerms];   // of tokens gr, of tokens gr + 8
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            float x[kLR][2];   // p s as it enters
-#pragma unroll
-            for (int r = 0; r < kLR; ++r) {
-              x[r][0] = weight_of(u, n, r, g, 0) * unit_of[n][r][g];
-              x[r][1] = weight_of(u, n, r, g, 1) * unit_of[n][r][g];
-              if constexpr (kMasked) {   // (a token that this row does not see need not be a number)
-                const int vis = sees(row_of(n, r)) - pos - u * kSet * kTile;
-                if (vis > 0) z[n][r][g] = fmaf(p[u][n][r][0], mid0, z[n][r][g]);
-                if (vis > 8) z[n][r][g] = fmaf(p[u][n][r][1], mid1, z[n][r][g]);
-              } else {
-                z[n][r][g] = fmaf(p[u][n][r][1], mid1, fmaf(p[u][n][r][0], mid0, z[n][r][g]));
-              }
-            }
-            if constexpr (T == 2) {   // its upper eleven bits and the rest, side by side in the row's two columns
-              const float x0 = x[0][0], x1 = x[0][1];
-              const float h0 = __uint_as_float(__float_as_uint(x0) & 0xFFFFE000u), h1 = __uint_as_float(__float_as_uint(x1) & 0xFFFFE000u);
-              b0[n][0] = pack_half2(h0, x0 - h0);
-              b1[n][0] = pack_half2(h1, x1 - h1);
-            } else {
-              auto term = [&](int e, uint32_t& first, uint32_t& second) {   // to nearest, and what is left
-                first = pack_half2(x[0][e], x[kLR - 1][e]);
-                const float2 high = unpack_half2(first);
-                if (kTerms == 2) second = pack_half2(x[0][e] - high.x, x[kLR - 1][e] - high.y);
-              };
-              term(0, b0[n][0], b0[n][kTerms - 1]);
-              term(1, b1[n][0], b1[n][kTerms - 1]);
-            }
-#pragma unroll
-            for (int y = 0; y < kTerms; ++y) {
-              b0[n][y] = transpose8x8(b0[n][y]);
-              b1[n][y] = transpose8x8(b1[n][y]);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < kSet; ++i) {
-            const uint4 w = lds128(v_at + my_codes + ((u * kSet + i) * C::kStride + g * kBlockBytes));
-            const uint32_t x8 = w.x >> 8, y8 = w.y >> 8, z8 = w.z >> 8, w8 = w.w >> 8;
-            const uint32_t A[4][4] = {{centred<false>(w.x), centred<false>(w.y), centred<false>(w.z), centred<false>(w.w)},
-                                      {centred<true>(w.x), centred<true>(w.y), centred<true>(w.z), centred<true>(w.w)},
-                                      {centred<false>(x8), centred<false>(y8), centred<false>(z8), centred<false>(w8)},
-                                      {centred<true>(x8), centred<true>(y8), centred<true>(z8), centred<true>(w8)}};
+          for (int g = 0; g < G; ++g) {
+            const float mid0 = unpack_half2(pv[u][g].x).y, mid1 = unpack_half2(pv[u][g].y).y;
+            uint32_t b0[NT][kTerms], b1[NT][kTerms];   // of tokens gr, of tokens gr + 8
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
+              float x[kLR][2];   // p s as it enters
+#pragma unroll
+              for (int r = 0; r < kLR; ++r) {
+                x[r][0] = weight_of(u, n, r, g, 0) * unit_of[n][r][g];
+                x[r][1] = weight_of(u, n, r, g, 1) * unit_of[n][r][g];
+                if constexpr (kMasked) {   // (a token that this row does not see need not be a number)
+                  const int vis = sees(row_of(n, r)) - pos - u * kSet * kTile;
+                  if (vis > 0) z[n][r][g] = fmaf(p[u][n][r][0], mid0, z[n][r][g]);
+                  if (vis > 8) z[n][r][g] = fmaf(p[u][n][r][1], mid1, z[n][r][g]);
+                } else {
+                  z[n][r][g] = fmaf(p[u][n][r][1], mid1, fmaf(p[u][n][r][0], mid0, z[n][r][g]));
+                }
+              }
+              if constexpr (T == 2) {   // its upper eleven bits and the rest, side by side in the row's two columns
+                const float x0 = x[0][0], x1 = x[0][1];
+                const float h0 = __uint_as_float(__float_as_uint(x0) & 0xFFFFE000u), h1 = __uint_as_float(__float_as_uint(x1) & 0xFFFFE000u);
+                b0[n][0] = pack_half2(h0, x0 - h0);
+                b1[n][0] = pack_half2(h1, x1 - h1);
+              } else {
+                auto term = [&](int e, uint32_t& first, uint32_t& second) {   // to nearest, and what is left
+                  first = pack_half2(x[0][e], x[kLR - 1][e]);
+                  const float2 high = unpack_half2(first);
+                  if (kTerms == 2) second = pack_half2(x[0][e] - high.x, x[kLR - 1][e] - high.y);
+                };
+                term(0, b0[n][0], b0[n][kTerms - 1]);
+                term(1, b1[n][0], b1[n][kTerms - 1]);
+              }
 #pragma unroll
               for (int y = 0; y < kTerms; ++y) {
-                const uint32_t c0 = kSet == 1 ? b0[n][y] : b0[n][y] & only[i], c1 = kSet == 1 ? b1[n][y] : b1[n][y] & only[i];
+                b0[n][y] = transpose8x8(b0[n][y]);
+                b1[n][y] = transpose8x8(b1[n][y]);
+              }
+            }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) mma_f16(O[n][g][k], A[k][0], A[k][1], A[k][2], A[k][3], c0, c1);
+            for (int i = 0; i < kSet; ++i) {
+              const uint4 w = lds128(v_at + my_codes + ((u * kSet + i) * C::kStride + g * kBlockBytes));
+              const uint32_t x8 = w.x >> 8, y8 = w.y >> 8, z8 = w.z >> 8, w8 = w.w >> 8;
+              const uint32_t A[4][4] = {{centred<false>(w.x), centred<false>(w.y), centred<false>(w.z), centred<false>(w.w)},
+                                        {centred<true>(w.x), centred<true>(w.y), centred<true>(w.z), centred<true>(w.w)},
+                                        {centred<false>(x8), centred<false>(y8), centred<false>(z8), centred<false>(w8)},
+                                        {centred<true>(x8), centred<true>(y8), centred<true>(z8), centred<true>(w8)}};
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int y = 0; y < kTerms; ++y) {
+                  const uint32_t c0 = kSet == 1 ? b0[n][y] : b0[n][y] & only[i], c1 = kSet == 1 ? b1[n][y] : b1[n][y] & only[i];
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) mma_f16(O[n][g][k], A[k][0], A[k][1], A[k][2], A[k][3], c0, c1);
+                }
               }
             }
           }
-        }
         }
       };
 
