@@ -865,8 +865,9 @@ __global__ void __launch_bounds__(Cfg<G, kColumns<kType>, L, NT>::kThreads, 1) k
 #pragma unroll
                 for (int e = 0; e < 4; ++e) O[n][g][i][e] = 0.f;
             }
+            __syncwarp();   // (the eight lanes of a row share the word: all have read the one before)
 #pragma unroll
-            for (int r = 0; r < kLR; ++r) __stcg(maximum_at(n, r), m[n][r]);   // (by each lane that reads it)
+            for (int r = 0; r < kLR; ++r) __stcg(maximum_at(n, r), m[n][r]);
           }
         }
       }
